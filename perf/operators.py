@@ -338,30 +338,30 @@ def _own_map(s):
 
 
 def _cache(s, abi):
-    return abi.ssd_kv8(s["k_codes"], s["v_codes"], s["k_scale"], s["v_scale"], s["n_pages"], s["hk"],
+    return abi.ssd_cache(s["k_codes"], s["v_codes"], s["k_scale"], s["v_scale"], s["n_pages"], s["hk"],
                        s["ps"], s["dh"])
 
 
 def _own_store(s):
     from paper_2510_22641_amd import ssd as abi
     kv, st, dt, ld, n = _cache(s, abi), _stream(), _dtype(s, abi), s["hk"] * s["dh"], s["n_pages"]
-    abi.ssd_kv8_store(kv, s["rows"], s["slot"], s["k"], s["v"], ld, dt, s["status"], st)
-    abi.ssd_kv8_load(kv, s["read"].numel(), s["read"], s["k_out"], s["v_out"], ld, dt, s["status"], st)
+    abi.ssd_cache_store(kv, s["rows"], s["slot"], s["k"], s["v"], ld, dt, s["status"], st)
+    abi.ssd_cache_load(kv, s["read"].numel(), s["read"], s["k_out"], s["v_out"], ld, dt, s["status"], st)
     return {"k": s["k_out"], "v": s["v_out"], "k_scale": s["k_scale"][:n], "v_scale": s["v_scale"][:n]}
 
 
 def _own_attend(s):
     from paper_2510_22641_amd import ssd as abi
     kv, ld = _cache(s, abi), s["hq"] * s["dh"]
-    a = abi.ssd_kv8_attn(B=s["B"], rows=s["rows"], max_rows=s["max_new"], max_len=s["max_len"],
+    a = abi.ssd_cache_attn(B=s["B"], rows=s["rows"], max_rows=s["max_new"], max_len=s["max_len"],
                          n_q_heads=s["hq"], dtype=_dtype(s, abi), q=s["q"], ldq=ld, out=s["out"], ldo=ld,
                          row_start=s["row_start"], seq_len=s["seq_len"], page_table=s["page_table"],
                          max_pages=s["max_pages"], bias=s["bias"],
                          n_bias=s["max_len"] if s["bias"] is not None else 0, scale=s["scale"],
                          status=s["status"])
     if s["workspace"] is None:  # a program sizes its workspace once
-        s["workspace"] = torch.empty(abi.ssd_kv8_attention_workspace(kv, a), dtype=torch.uint8, device="cuda")
-    abi.ssd_kv8_attention(kv, a, s["workspace"], s["workspace"].numel(), _stream())
+        s["workspace"] = torch.empty(abi.ssd_cache_attention_workspace(kv, a), dtype=torch.uint8, device="cuda")
+    abi.ssd_cache_attention(kv, a, s["workspace"], s["workspace"].numel(), _stream())
     return s["out"]
 
 
