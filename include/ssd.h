@@ -60,7 +60,12 @@ enum {
 };
 
 /* device status bits (ssd_sync_status; ssd_generate returns SSD_ERR_DEVICE when one is set) */
-enum { SSD_DEV_BAD_TOKEN = 1, SSD_DEV_CAPACITY = 2, SSD_DEV_BAD_PAGE = 4 };
+enum {
+  SSD_DEV_BAD_TOKEN = 1,
+  SSD_DEV_CAPACITY = 2,
+  SSD_DEV_BAD_PAGE = 4,
+  SSD_DEV_NOT_FINITE = 8 /* a row stored in 8 bits held an infinity or a NaN */
+};
 
 /* Decoder and context dimensions, copied at ssd_create. */
 typedef struct {
@@ -339,6 +344,94 @@ int ssd_read_bandwidth(const void* d_buf, size_t bytes, float* d_out, int reps, 
 /* Synchronise the stream; SSD_OK, SSD_ERR_HIP, or SSD_ERR_DEVICE when the device status word is
  * non-zero (then *status, if not NULL, receives the SSD_DEV_* bits) — and clear the word. */
 int ssd_sync_status(ssd_ctx* ctx, int32_t* status);
+
+/* ---- The 8-bit paged cache ---------------------------------------------------------------
+ *
+ * Keys and values of one layer as int8 codes in pages, with one float32 scale for each page and
+ * head (a block): value = code * scale.  These calls need no context; a context whose kvdtype is
+ * SSD_I8 makes them itself.  They are asynchronous on `stream` (a hipStream_t; NULL: the null
+ * stream of the current device) and may be captured into a graph; the pointers belong to the
+ * stream's device, whichever device is current.  d_status is one device word of the caller's, into
+ * which SSD_DEV_* bits are set and which no call clears. */
+typedef struct {
+  void* k_codes;     /* int8 [n_pages][n_heads][page_size][d_head], 16-byte aligned */
+  void* v_codes;     /* same */
+  float* k_scale;    /* [n_pages][n_heads] */
+  float* v_scale;    /* same */
+  int32_t n_pages;
+  int32_t n_heads;   /* heads of the cache; the queries may have a multiple of them */
+  int32_t page_size; /* 1 .. 256 positions */
+  int32_t d_head;    /* 64 or 128 */
+} ssd_cache;
+
+/* Page table and slot map of a step from the requests' lengths.  Sequence b holds d_seq_len[b]
+ * positions and receives d_new[b] more (0 for none).  New pages, ceil((len + new) / page_size) -
+ * ceil(len / page_size) of them, are taken from the front of d_free [n_free], sequences in order,
+ * and entered into row b of d_page_table [B][max_pages] behind those it has; other entries stay as
+ * they are, and *d_taken receives the pages taken.  d_free NULL (n_free 0): the table has the pages
+ * already and is only read.  d_row_start [B + 1] receives the first row of each sequence, its new
+ * positions being consecutive rows, and their total; d_slot [max_rows] the slot page * page_size +
+ * offset of each row, -1 for rows behind the last.  1 <= B <= 4096.  A negative count, a length
+ * outside the table, rows past max_rows (cut) or pages past n_free (table entries -1) set
+ * SSD_DEV_CAPACITY, a page outside [0, n_pages) SSD_DEV_BAD_PAGE; the rows concerned get slot -1. */
+int ssd_page_map(int B, int page_size, int n_pages, int max_pages, const int32_t* d_seq_len,
+                 const int32_t* d_new, const int32_t* d_free, int n_free, int32_t* d_page_table,
+                 int32_t* d_row_start, int64_t* d_slot, int max_rows, int32_t* d_taken,
+                 int32_t* d_status, void* stream);
+
+/* Store rows of keys and values into their blocks: row r, head h, dimension d at r * ld + h *
+ * d_head + d of d_k and d_v (elements of dtype, SSD_F32 or SSD_BF16; ld >= n_heads * d_head),
+ * into slot d_slot[r] (-1: the row is skipped).  A run, rows on consecutive slots of one page, is
+ * stored at once: beginning at offset o it keeps the o rows in front of it, starts the block anew
+ * when o = 0, and leaves what is behind it without meaning.  Runs on one page follow one another in
+ * the call, as ssd_page_map lays them, and are stored in that order; a page whose runs have another
+ * page's between them ends up with a mixture of them.  The block's scale
+ * becomes the smallest power of two s (at least 2^-100) such that 127 s covers its rows' largest
+ * magnitude, those in front rescaled; codes are the nearest whole numbers (ties to even).  8 bits
+ * hold neither infinities nor NaN: SSD_DEV_NOT_FINITE is set, an infinity becomes the block's
+ * largest value, a NaN zero.  A slot outside the pools sets SSD_DEV_BAD_PAGE and is skipped. */
+int ssd_cache_store(const ssd_cache* cache, int rows, const int64_t* d_slot, const void* d_k,
+                    const void* d_v, int64_t ld, int dtype, int32_t* d_status, void* stream);
+
+/* The values of rows read back: d_k and d_v laid out as for ssd_cache_store receive code * scale
+ * of slot d_slot[r] (-1: the row is left as it is), in any order and as often as wanted. */
+int ssd_cache_load(const ssd_cache* cache, int rows, const int64_t* d_slot, void* d_k, void* d_v,
+                   int64_t ld, int dtype, int32_t* d_status, void* stream);
+
+/* Causal softmax attention over the cache.  Row j of sequence b sits at position p =
+ * seq_len[b] + pos_off + j and attends positions 0 .. p; scores q . k * scale + bias[h][min(p - i,
+ * n_bias - 1)] (no bias: NULL).  Query head h reads cache head h / (n_q_heads / n_heads).  A row
+ * without a position to attend, or whose scores are all -inf, gets zeros; a NaN score stays NaN in
+ * its own row.  Rows of no sequence are left as they are.  A position past the table sets
+ * SSD_DEV_CAPACITY (its keys end at the table's), as does a sequence of more than max_rows rows (the
+ * further ones are left); a page outside the pools SSD_DEV_BAD_PAGE, its keys skipped. */
+typedef struct {
+  int32_t B;          /* sequences, 1 .. 4096 */
+  int32_t rows;       /* query rows in all; B * max_rows when row_start is NULL */
+  int32_t max_rows;   /* most rows of one sequence */
+  int32_t max_len;    /* positions attended, at most (only the launch shape depends on it) */
+  int32_t n_q_heads;  /* a multiple of the cache's heads */
+  int32_t dtype;      /* SSD_F32 or SSD_BF16: q and out */
+  const void* q;      /* row r, head h at r * ldq + h * d_head */
+  int64_t ldq;
+  void* out;          /* row r, head h at r * ldo + h * d_head; not q */
+  int64_t ldo;
+  const int32_t* row_start;  /* [B + 1] first row of each sequence and their total, or NULL */
+  const int32_t* seq_len;    /* [B] */
+  int32_t pos_off;
+  int32_t max_pages;         /* columns of page_table; max_pages * page_size <= 2^24 */
+  const int32_t* page_table; /* [B][max_pages] */
+  const float* bias;         /* [n_q_heads][n_bias], or NULL */
+  int32_t n_bias;
+  float scale;
+  int32_t* status;
+} ssd_cache_attn;
+
+/* Bytes of workspace (256-byte aligned) a call with these sizes needs, 0 for none; the pointers are
+ * not looked at.  A call writes it before it reads it, so calls on one stream may share it. */
+size_t ssd_cache_attention_workspace(const ssd_cache* cache, const ssd_cache_attn* attn);
+int ssd_cache_attention(const ssd_cache* cache, const ssd_cache_attn* attn, void* d_workspace,
+                        size_t workspace_bytes, void* stream);
 
 /* Human-readable name of a return code. */
 const char* ssd_status_string(int code);

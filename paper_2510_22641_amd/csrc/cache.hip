@@ -1,0 +1,438 @@
+// The 8-bit paged cache: slot maps from request lengths, storing rows as codes, reading them back.
+//
+// A block is one page of one head: page_size rows of d_head int8 codes c with one scale s, a power
+// of two; the row's values are c s.  With the largest magnitude a of the block's rows, s is the
+// smallest 2^e (e >= -100) with a <= 127 2^e: dividing by it is exact, so a value is off by at most
+// half a code, s / 2 <= a / 127, and a block whose scale falls again is rescaled without loss.
+#include "device.h"
+#include "kernels.h"
+
+#include <cfloat>
+
+namespace ssd {
+
+namespace {
+
+constexpr int MAP_THREADS = 256;
+constexpr int MAP_ROWS = 1024;  // rows a block writes slots for
+
+// Exclusive prefix sums over the block's threads of one value each; *total receives the sum.
+__device__ __forceinline__ long long block_scan(long long v, long long* waves, long long* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  long long x = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const long long y = __shfl_up(x, o, SSD_WAVE);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();  // the previous use of waves[]
+  if (lane == 63) waves[wave] = x;
+  __syncthreads();
+  long long before = 0, sum = 0;
+#pragma unroll
+  for (int w = 0; w < MAP_THREADS / 64; ++w) {
+    if (w < wave) before += waves[w];
+    sum += waves[w];
+  }
+  *total = sum;
+  return before + x - v;
+}
+
+// Largest b in [0, B) with start[b] <= r (start[0] = 0, non-decreasing).
+__device__ __forceinline__ int find_seq(const int* start, int B, int r) {
+  int lo = 0, hi = B;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (start[mid] <= r) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// Slot map and page table of B <= PAGE_MAP_MAX_BATCH sequences.  Every block repeats the two prefix
+// sums over the sequences (a few loads a thread), so that one launch does it all: no block waits for
+// another, and a new page's id comes from the free list by its rank instead of from the table that
+// other blocks are writing.  Then a block writes its share of the new table entries and the slots
+// of its MAP_ROWS rows, each finding its sequence by bisection in LDS.  Bound: launch latency and
+// one dependent chain (lengths, sums, table entry), not bytes.
+__global__ __launch_bounds__(MAP_THREADS) void page_map_kernel(const PageMapArgs a) {
+  extern __shared__ int map_lds[];
+  int* row0 = map_lds;               // [B + 1] first row of each sequence
+  int* page0 = map_lds + a.B + 1;    // [B + 1] rank in the free list of its first new page
+  __shared__ long long waves[MAP_THREADS / 64];
+  const int tid = threadIdx.x;
+  const long long cap = (long long)a.max_pages * a.page_size;
+  int fault = 0;
+  // pages of a sequence with `len` positions held and n new rows: [first, end) of its table row
+  auto need = [&](int len, int n, int& first) {
+    first = 0;
+    if (!a.free_pages || len < 0 || len > cap || n <= 0) return 0;
+    first = (len + a.page_size - 1) / a.page_size;
+    const long long end = (long long)len + n < cap ? (long long)len + n : cap;
+    return (int)((end + a.page_size - 1) / a.page_size) - first;
+  };
+  long long rows = 0, pages = 0;
+  for (int b0 = 0; b0 < a.B; b0 += MAP_THREADS) {
+    const int b = b0 + tid;
+    int len = 0, n = 0;
+    if (b < a.B) {
+      len = a.seq_len[b] + a.pos_off;
+      n = a.new_rows ? a.new_rows[b] : a.new_const;
+      if (n < 0) { n = 0; fault = 1; }
+      if (len < 0 || (long long)len + n > cap) fault |= n > 0;
+    }
+    long long sum;
+    const long long r0 = rows + block_scan(n, waves, &sum);
+    rows += sum;
+    // rows past max_rows are cut: they get no slot and no page
+    const int r_lo = (int)(r0 < a.max_rows ? r0 : a.max_rows);
+    const int r_hi = (int)(r0 + n < a.max_rows ? r0 + n : a.max_rows);
+    int first;
+    const long long p0 = pages + block_scan(need(len, r_hi - r_lo, first), waves, &sum);
+    pages += sum;
+    if (b < a.B) {
+      row0[b] = r_lo;
+      page0[b] = (int)(p0 < a.n_free ? p0 : a.n_free);
+    }
+  }
+  if (rows > a.max_rows || pages > a.n_free) fault = 1;
+  const int n_rows = (int)(rows < a.max_rows ? rows : a.max_rows);
+  const int n_pages = (int)(pages < a.n_free ? pages : a.n_free);
+  if (tid == 0) {
+    row0[a.B] = n_rows;
+    page0[a.B] = n_pages;
+  }
+  __syncthreads();
+  if (blockIdx.x == 0) {
+    if (a.row_start)
+      for (int b = tid; b <= a.B; b += MAP_THREADS) a.row_start[b] = row0[b];
+    if (tid == 0 && a.taken) *a.taken = n_pages;
+    if (fault) atomicOr(a.status, SSD_DEV_CAPACITY);
+  }
+  // new table entries: rank t of the free list belongs to the sequence with page0[b] <= t
+  for (int t = blockIdx.x * MAP_THREADS + tid; t < n_pages; t += gridDim.x * MAP_THREADS) {
+    const int b = find_seq(page0, a.B, t);
+    int first;
+    need(a.seq_len[b] + a.pos_off, row0[b + 1] - row0[b], first);
+    a.page_table[(size_t)b * a.max_pages + first + t - page0[b]] = a.free_pages[t];
+  }
+  // entries that the free list could not fill: the last sequences' (none unless `fault`)
+  if (a.free_pages && pages > a.n_free && blockIdx.x == 0) {
+    for (int b = tid; b < a.B; b += MAP_THREADS) {
+      int first;
+      const int n = need(a.seq_len[b] + a.pos_off, row0[b + 1] - row0[b], first);
+      for (int i = page0[b + 1] - page0[b]; i < n; ++i) a.page_table[(size_t)b * a.max_pages + first + i] = -1;
+    }
+  }
+  if (!a.slot) return;
+#pragma unroll
+  for (int u = 0; u < MAP_ROWS / MAP_THREADS; ++u) {
+    const int r = blockIdx.x * MAP_ROWS + u * MAP_THREADS + tid;
+    if (r >= a.max_rows) break;
+    int64_t s = -1;
+    if (r < n_rows) {
+      const int b = find_seq(row0, a.B, r);
+      const int len = a.seq_len[b] + a.pos_off;
+      const long long p = (long long)len + r - row0[b];
+      if (len >= 0 && p < cap) {
+        const int i = (int)(p / a.page_size);
+        int first;
+        const int n = need(len, row0[b + 1] - row0[b], first);
+        int page;
+        if (a.free_pages && i >= first && n > 0) {
+          const int t = page0[b] + i - first;
+          page = t < page0[b + 1] ? a.free_pages[t] : -1;
+        } else {
+          page = a.page_table[(size_t)b * a.max_pages + i];
+          if (page < 0) atomicOr(a.status, SSD_DEV_BAD_PAGE);
+        }
+        if (page >= a.n_pages) {
+          atomicOr(a.status, SSD_DEV_BAD_PAGE);
+          page = -1;
+        }
+        if (page >= 0) s = (int64_t)page * a.page_size + p % a.page_size;
+      }
+    }
+    a.slot[r] = s;
+  }
+}
+
+// Four consecutive elements of a row; VEC: the row is aligned for one load.
+template <typename T, bool VEC>
+__device__ __forceinline__ float4 load4(const T* p) {
+  if constexpr (!VEC) return make_float4(load_elem(p), load_elem(p + 1), load_elem(p + 2), load_elem(p + 3));
+  else if constexpr (sizeof(T) == 4) return *reinterpret_cast<const float4*>(p);
+  else {
+    const uint2 r = *reinterpret_cast<const uint2*>(p);
+    return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u),
+                       __uint_as_float(r.y << 16), __uint_as_float(r.y & 0xffff0000u));
+  }
+}
+
+// |v| where it is finite, else 0; `bad` collects whether any was not.
+__device__ __forceinline__ float finite_abs(float v, bool& bad) {
+  const float m = fabsf(v);
+  if (m <= FLT_MAX) return m;
+  bad = true;
+  return 0.f;
+}
+
+// Exponent e >= -100 of the smallest scale 2^e with top <= 127 2^e (top >= 0, finite).
+__device__ __forceinline__ int scale_exp(float top) {
+  const uint32_t u = __float_as_uint(top);
+  const int e = (int)(u >> 23) - 133 + ((u & 0x7fffffu) > 0x7e0000u ? 1 : 0);  // 127 = 1.984375 2^6
+  return e < -100 ? -100 : e;
+}
+
+// The code of x = v * 2^-e: nearest (even), an infinity the largest, a NaN zero.
+__device__ __forceinline__ uint32_t code_of(float x) {
+  const float r = fminf(fmaxf(rintf(x), -127.f), 127.f);
+  return (uint32_t)(int)(x == x ? r : 0.f) & 255u;
+}
+
+__device__ __forceinline__ uint32_t codes_of(const float4& v, float inv) {
+  return code_of(v.x * inv) | code_of(v.y * inv) << 8 | code_of(v.z * inv) << 16 | code_of(v.w * inv) << 24;
+}
+
+__device__ __forceinline__ float code_at(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
+
+constexpr int STORE_WAVES = 4;
+constexpr int STORE_HELD = 8;  // passes of rows kept in registers between the maximum and the codes
+
+// Rows into their blocks.  A run is the rows on consecutive slots of one page; a wave owns, for one
+// head of K or V, the stretches of rows on one page (rows without a slot do not interrupt them) that
+// begin in `window` consecutive rows, and stores a stretch's runs one after the other.  For a run it
+// takes the largest magnitude over the run and over the rows the block already holds in front of it
+// (their codes times the old scale), rescales those where the block's scale changes, and writes the
+// run's codes; 32 (or 16) lanes take four elements each of a row.  Every block belongs to one wave,
+// so nothing is atomic.  Bound: bytes for long prompts; the chain slot -> rows, codes and scale ->
+// reduction -> store for single tokens.
+template <typename T, int DH, bool VEC>
+__global__ __launch_bounds__(64 * STORE_WAVES) void cache_store_kernel(const CacheRowsArgs a, const int window) {
+  constexpr int LPR = DH / 4, RPP = 64 / LPR;  // lanes a row, rows a pass
+  const int lane = threadIdx.x & 63;
+  const int task = __builtin_amdgcn_readfirstlane(blockIdx.y * STORE_WAVES + (threadIdx.x >> 6));
+  if (task >= 2 * a.n_heads) return;  // whole waves
+  const bool is_v = task >= a.n_heads;
+  const int h = is_v ? task - a.n_heads : task;
+  const int ps = a.page_size;
+  const int64_t n_slots = (int64_t)a.n_pages * ps;
+  const T* src = reinterpret_cast<const T*>(is_v ? a.v : a.k) + (size_t)h * DH + (lane % LPR) * 4;
+  int8_t* codes = is_v ? a.v_codes : a.k_codes;
+  float* scales = is_v ? a.v_scale : a.k_scale;
+  const int lr = lane / LPR, lc = (lane % LPR) * 4;
+  // the stretches that begin in this window
+  const int w0 = blockIdx.x * window, w1 = min(w0 + window, a.rows);
+  auto fits = [&](int64_t v) { return v >= 0 && v < n_slots; };
+  int64_t mine = -1;
+  bool first = false, back = false;
+  {
+    const int r = w0 + lane;
+    if (r < w1) {
+      mine = a.slot[r];
+      const int64_t prev = r > 0 ? a.slot[r - 1] : -1;
+      if (fits(mine)) {
+        first = r == 0 || (fits(prev) && prev / ps != mine / ps);
+        back = r > 0 && !fits(prev);
+      } else if (mine != -1 && task == 0) {
+        atomicOr(a.status, SSD_DEV_BAD_PAGE);
+      }
+    }
+  }
+  uint64_t starts = __ballot(first), backs = __ballot(back);
+  while (backs) {  // behind a row without a slot: the nearest row that has one decides
+    const int at = __builtin_ctzll(backs);
+    backs &= backs - 1;
+    const int64_t page = __shfl(mine, at, SSD_WAVE) / ps;
+    bool own = true;
+    for (int e = w0 + at - 2; e >= 0; e -= 64) {
+      const int64_t v = e - lane >= 0 ? a.slot[e - lane] : -1;
+      const uint64_t m = __ballot(fits(v));
+      if (m) {
+        own = __shfl(v, __builtin_ctzll(m), SSD_WAVE) / ps != page;
+        break;
+      }
+    }
+    if (own) starts |= 1ull << at;
+  }
+  bool bad = false;
+  int r0 = -1, page = -1;  // the next run, of the current stretch where r0 >= 0
+  int64_t s0 = 0;
+  while (r0 >= 0 || starts) {
+    if (r0 < 0) {
+      const int at = __builtin_ctzll(starts);
+      starts &= starts - 1;
+      r0 = w0 + at;
+      s0 = __shfl(mine, at, SSD_WAVE);
+      page = (int)(s0 / ps);
+    }
+    const int off = (int)(s0 - (int64_t)page * ps), run = r0;
+    // rows of the run, up to the page's end, and the row with a slot that follows it
+    int n = 0;
+    int64_t next = -1;
+    r0 = -1;
+    for (int e = run; e < a.rows; e += 64) {
+      const int64_t v = e + lane < a.rows ? a.slot[e + lane] : -1;
+      const int i = e + lane - run;
+      const uint64_t in = __ballot(i == n + lane && off + i < ps && v == s0 + i);
+      const int k = ~in ? __builtin_ctzll(~in) : 64;
+      n += k;
+      const uint64_t more = __ballot(lane >= k && fits(v));
+      if (more) {
+        const int at = __builtin_ctzll(more);
+        next = __shfl(v, at, SSD_WAVE);
+        if (next / ps == page) r0 = e + at;
+        break;
+      }
+    }
+    int8_t* block = codes + ((size_t)page * a.n_heads + h) * ps * DH;
+    float* sp = scales + (size_t)page * a.n_heads + h;
+    const float s_old = off ? *sp : 0.f;
+    float top = 0.f;
+    float4 kept[STORE_HELD];
+#pragma unroll
+    for (int p = 0; p < STORE_HELD; ++p) {
+      if (p * RPP < n) {  // uniform
+        const int r = p * RPP + lr;
+        kept[p] = load4<T, VEC>(src + (size_t)(run + min(r, n - 1)) * a.ld);
+      }
+    }
+    float held = 0.f;
+    for (int r = lr; r < off; r += RPP) {
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(block + (size_t)r * DH + lc);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) held = fmaxf(held, fabsf(code_at(w, i)));
+    }
+    bool ignored = false;  // a stored scale that is not finite counts as zero
+    top = finite_abs(held * s_old, ignored);
+#pragma unroll
+    for (int p = 0; p < STORE_HELD; ++p) {
+      if (p * RPP < n) {  // (a row past the run repeats its last: no other maximum)
+        top = fmaxf(fmaxf(top, finite_abs(kept[p].x, bad)), finite_abs(kept[p].y, bad));
+        top = fmaxf(fmaxf(top, finite_abs(kept[p].z, bad)), finite_abs(kept[p].w, bad));
+      }
+    }
+    for (int r = STORE_HELD * RPP + lr; r < n; r += RPP) {
+      const float4 v = load4<T, VEC>(src + (size_t)(run + r) * a.ld);
+      top = fmaxf(fmaxf(top, finite_abs(v.x, bad)), finite_abs(v.y, bad));
+      top = fmaxf(fmaxf(top, finite_abs(v.z, bad)), finite_abs(v.w, bad));
+    }
+    const int e = scale_exp(wave_max(top));
+    const float s_new = __uint_as_float((uint32_t)(e + 127) << 23);
+    const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+    if (off && s_new != s_old) {
+      for (int r = lr; r < off; r += RPP) {
+        uint32_t* p = reinterpret_cast<uint32_t*>(block + (size_t)r * DH + lc);
+        const uint32_t w = *p;
+        *p = codes_of(make_float4(code_at(w, 0) * s_old, code_at(w, 1) * s_old, code_at(w, 2) * s_old,
+                                  code_at(w, 3) * s_old), inv);
+      }
+    }
+    uint32_t* dst = reinterpret_cast<uint32_t*>(block + (size_t)off * DH + lc);
+#pragma unroll
+    for (int p = 0; p < STORE_HELD; ++p) {
+      const int r = p * RPP + lr;
+      if (r < n) dst[(size_t)r * LPR] = codes_of(kept[p], inv);
+    }
+    for (int r = STORE_HELD * RPP + lr; r < n; r += RPP)
+      dst[(size_t)r * LPR] = codes_of(load4<T, VEC>(src + (size_t)(run + r) * a.ld), inv);
+    if (lane == 0) *sp = s_new;
+    if (r0 >= 0) {  // another run on this page, which reads what was just written
+      s0 = next;
+      __threadfence_block();
+    }
+  }
+  if (__any(bad) && lane == 0) atomicOr(a.status, SSD_DEV_NOT_FINITE);
+}
+
+// Rows back from their blocks: eight codes a lane, consecutive lanes on consecutive elements of a
+// row, K (blockIdx.y 0) or V.  Bound: bytes.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void cache_load_kernel(const CacheRowsArgs a) {
+  const int per = a.n_heads * a.d_head / 8;  // lanes a row
+  const size_t t = (size_t)blockIdx.x * 256 + threadIdx.x;
+  const size_t r = t / per;
+  if (r >= (size_t)a.rows) return;
+  const int c = (int)(t - r * per) * 8, h = c / a.d_head;
+  const bool is_v = blockIdx.y;
+  const int64_t s = a.slot[r];
+  if (s < 0 || s >= (int64_t)a.n_pages * a.page_size) {
+    if (s != -1) atomicOr(a.status, SSD_DEV_BAD_PAGE);
+    return;
+  }
+  const int64_t page = s / a.page_size, off = s - page * a.page_size;
+  const size_t block = (size_t)page * a.n_heads + h;
+  const int8_t* p = (is_v ? a.v_codes : a.k_codes) + (block * a.page_size + off) * a.d_head + (c - h * a.d_head);
+  const uint2 w = *reinterpret_cast<const uint2*>(p);
+  const float sc = (is_v ? a.v_scale : a.k_scale)[block];
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[i] = code_at(w.x, i) * sc;
+    f[4 + i] = code_at(w.y, i) * sc;
+  }
+  T* o = reinterpret_cast<T*>(is_v ? a.v_out : a.k_out) + r * a.ld + c;
+  if constexpr (!VEC) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) store_elem(o + i, f[i]);
+  } else if constexpr (sizeof(T) == 4) {
+    reinterpret_cast<float4*>(o)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    reinterpret_cast<float4*>(o)[1] = make_float4(f[4], f[5], f[6], f[7]);
+  } else {
+    *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]),
+                                              pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+  }
+}
+
+bool aligned(const void* p, int64_t ld, size_t elem, size_t bytes) {
+  return reinterpret_cast<uintptr_t>(p) % bytes == 0 && ((size_t)ld * elem) % bytes == 0;
+}
+
+template <typename T>
+hipError_t store_t(const CacheRowsArgs& a, int window, dim3 grid, hipStream_t s) {
+  const bool vec = aligned(a.k, a.ld, sizeof(T), 4 * sizeof(T)) && aligned(a.v, a.ld, sizeof(T), 4 * sizeof(T));
+  const dim3 block(64 * STORE_WAVES);
+  if (a.d_head == 64) {
+    if (vec) hipLaunchKernelGGL((cache_store_kernel<T, 64, true>), grid, block, 0, s, a, window);
+    else hipLaunchKernelGGL((cache_store_kernel<T, 64, false>), grid, block, 0, s, a, window);
+  } else {
+    if (vec) hipLaunchKernelGGL((cache_store_kernel<T, 128, true>), grid, block, 0, s, a, window);
+    else hipLaunchKernelGGL((cache_store_kernel<T, 128, false>), grid, block, 0, s, a, window);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_page_map(const PageMapArgs& a, hipStream_t s) {
+  if (a.B < 1 || a.B > PAGE_MAP_MAX_BATCH) return hipErrorInvalidValue;
+  const int blocks = a.max_rows > MAP_ROWS ? (a.max_rows + MAP_ROWS - 1) / MAP_ROWS : 1;
+  hipLaunchKernelGGL(page_map_kernel, dim3(blocks), dim3(MAP_THREADS), 2 * (a.B + 1) * sizeof(int), s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_store(const CacheRowsArgs& a, hipStream_t s) {
+  if (a.rows < 1) return hipSuccess;
+  // One row a wave while that leaves the device room; long prompts 16, a usual page's worth, since
+  // most waves of one row would find that their row begins no run.
+  const int window = a.rows > 256 ? 16 : 1;
+  const dim3 grid((a.rows + window - 1) / window, (2 * a.n_heads + STORE_WAVES - 1) / STORE_WAVES);
+  return a.dtype == 1 ? store_t<bf16_t>(a, window, grid, s) : store_t<float>(a, window, grid, s);
+}
+
+hipError_t launch_cache_load(const CacheRowsArgs& a, hipStream_t s) {
+  if (a.rows < 1) return hipSuccess;
+  const size_t lanes = (size_t)a.rows * (a.n_heads * a.d_head / 8);
+  const dim3 grid((unsigned)((lanes + 255) / 256), 2), block(256);
+  const size_t elem = a.dtype == 1 ? 2 : 4;
+  const bool vec = aligned(a.k_out, a.ld, elem, 16) && aligned(a.v_out, a.ld, elem, 16);
+  if (a.dtype == 1) {
+    if (vec) hipLaunchKernelGGL((cache_load_kernel<bf16_t, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((cache_load_kernel<bf16_t, false>), grid, block, 0, s, a);
+  } else {
+    if (vec) hipLaunchKernelGGL((cache_load_kernel<float, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((cache_load_kernel<float, false>), grid, block, 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace ssd

@@ -364,5 +364,74 @@ hipError_t launch_gen_init(const GenInitArgs& a, hipStream_t s);
 hipError_t launch_bias_table(const float* rel_bias, const int32_t* bucket, int H, int max_seq,
                              float* table, hipStream_t s);
 
+// ---- the 8-bit paged cache (cache.hip, cache_attention.hip) ----
+
+constexpr int PAGE_MAP_MAX_BATCH = 4096;  // two prefix sums over the sequences in LDS
+constexpr int CACHE_MAX_PAGE = 256;       // positions per page
+constexpr int CACHE_SPLITS_MAX = 64;
+
+struct PageMapArgs {
+  int B, page_size, n_pages, max_pages;
+  const int32_t* seq_len;   // [B]; positions held: seq_len[b] + pos_off
+  int pos_off;
+  const int32_t* new_rows;  // [B], or null: new_const each
+  int new_const;
+  const int32_t* free_pages;  // [n_free], or null: the table has every page already
+  int n_free;
+  int32_t* page_table;      // [B][max_pages]
+  int32_t* row_start;       // [B + 1] or null
+  int64_t* slot;            // [max_rows] or null
+  int max_rows;
+  int32_t* taken;           // [1] or null
+  int32_t* status;
+};
+hipError_t launch_page_map(const PageMapArgs& a, hipStream_t s);
+
+// Rows in (k, v) or out (k_out, v_out): row r, head h, dimension d at r ld + h d_head + d.
+struct CacheRowsArgs {
+  int8_t* k_codes;  // [n_pages][n_heads][page_size][d_head]
+  int8_t* v_codes;
+  float* k_scale;   // [n_pages][n_heads]
+  float* v_scale;
+  int n_pages, n_heads, page_size, d_head;
+  int rows;
+  const int64_t* slot;  // [rows]
+  const void* k;
+  const void* v;
+  void* k_out;
+  void* v_out;
+  int64_t ld;
+  int dtype;
+  int32_t* status;
+};
+hipError_t launch_cache_store(const CacheRowsArgs& a, hipStream_t s);
+hipError_t launch_cache_load(const CacheRowsArgs& a, hipStream_t s);
+
+struct CacheAttnArgs {
+  const int8_t* k_codes;
+  const int8_t* v_codes;
+  const float* k_scale;
+  const float* v_scale;
+  int n_pages, n_heads, page_size, d_head;
+  int B, rows, max_rows, max_len, n_q_heads, dtype;
+  const void* q;  // row r, head h at r ldq + h d_head
+  int64_t ldq;
+  void* out;
+  int64_t ldo;
+  bool out_vec;              // rows of out are aligned for four elements a store
+  const int32_t* row_start;  // [B + 1], or null: max_rows rows each
+  const int32_t* seq_len;
+  int pos_off;
+  const int32_t* page_table;
+  int max_pages;
+  const float* bias;  // [n_q_heads][n_bias] or null
+  int n_bias;
+  float scale;
+  int32_t* status;
+  float* part;        // cache_attn_part_floats of them
+};
+int cache_attn_splits(const CacheAttnArgs& a);
+size_t cache_attn_part_floats(const CacheAttnArgs& a);
+hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t s);
 
 }  // namespace ssd

@@ -841,6 +841,86 @@ int init_ctx(ssd_ctx* c, const ssd_dims& d, const ssd_weights* w, const ssd_kv* 
   return SSD_OK;
 }
 
+// The stream's device as the current one while a context-free call launches on it.
+struct StreamDevice {
+  int before = -1;
+  bool ok = true;
+  explicit StreamDevice(hipStream_t s) {
+    if (!s) return;  // the null stream is the current device's
+    int cur = -1, dev = -1;
+    ok = hipGetDevice(&cur) == hipSuccess && hipStreamGetDevice(s, &dev) == hipSuccess;
+    if (ok && dev != cur) {
+      ok = hipSetDevice(dev) == hipSuccess;
+      before = cur;
+    }
+  }
+  ~StreamDevice() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
+// Positions of a sequence the 8-bit cache's kernels index: page arithmetic holds to 2^24.
+bool cache_pages_ok(int page_size, int max_pages) {
+  return page_size >= 1 && page_size <= CACHE_MAX_PAGE && max_pages >= 1 &&
+         (long long)max_pages * page_size <= 1 << 24;
+}
+
+bool cache_shape_ok(const ssd_cache* c) {
+  return c->n_pages >= 1 && c->n_heads >= 1 && c->n_heads <= 4096 && c->page_size >= 1 &&
+         c->page_size <= CACHE_MAX_PAGE && (c->d_head == 64 || c->d_head == 128);
+}
+
+bool cache_pointers_ok(const ssd_cache* c) {
+  return c->k_codes && c->v_codes && c->k_scale && c->v_scale && (uintptr_t)c->k_codes % 16 == 0 &&
+         (uintptr_t)c->v_codes % 16 == 0 && (uintptr_t)c->k_scale % 4 == 0 && (uintptr_t)c->v_scale % 4 == 0;
+}
+
+template <typename A>
+void cache_fields(const ssd_cache* c, A& a) {
+  a.k_codes = reinterpret_cast<int8_t*>(c->k_codes);
+  a.v_codes = reinterpret_cast<int8_t*>(c->v_codes);
+  a.k_scale = c->k_scale;
+  a.v_scale = c->v_scale;
+  a.n_pages = c->n_pages;
+  a.n_heads = c->n_heads;
+  a.page_size = c->page_size;
+  a.d_head = c->d_head;
+}
+
+// Checks of ssd_cache_store and ssd_cache_load, and what their launches share.
+int cache_rows(const ssd_cache* cache, int rows, const int64_t* d_slot, const void* d_k, const void* d_v,
+               int64_t ld, int dtype, int32_t* d_status, CacheRowsArgs& a) {
+  if (!cache || !cache_pointers_ok(cache) || !d_status || rows < 0) return SSD_ERR_ARG;
+  if (!cache_shape_ok(cache) || rows > 1 << 24) return SSD_ERR_SHAPE;
+  if (dtype != SSD_F32 && dtype != SSD_BF16) return SSD_ERR_ARG;
+  if (ld < (int64_t)cache->n_heads * cache->d_head) return SSD_ERR_ARG;
+  const size_t elem = dtype == SSD_BF16 ? 2 : 4;
+  if (rows > 0 && (!d_slot || !d_k || !d_v || (uintptr_t)d_k % elem || (uintptr_t)d_v % elem)) return SSD_ERR_ARG;
+  cache_fields(cache, a);
+  a.rows = rows; a.slot = d_slot; a.ld = ld; a.dtype = dtype; a.status = d_status;
+  return SSD_OK;
+}
+
+// The sizes of an attention call, checked.
+int cache_attn_sizes(const ssd_cache* cache, const ssd_cache_attn* t, CacheAttnArgs& a) {
+  if (!cache || !t) return SSD_ERR_ARG;
+  if (!cache_shape_ok(cache) || !cache_pages_ok(cache->page_size, t->max_pages)) return SSD_ERR_SHAPE;
+  if (t->dtype != SSD_F32 && t->dtype != SSD_BF16) return SSD_ERR_ARG;
+  if (t->B < 1 || t->B > PAGE_MAP_MAX_BATCH || t->rows < 0 || t->rows > 1 << 24 || t->max_rows < 1 ||
+      t->max_rows > 1 << 24 || t->max_len < 1 || t->n_q_heads < 1 || t->n_q_heads > 4096 ||
+      t->n_q_heads % cache->n_heads)
+    return SSD_ERR_SHAPE;
+  if (!t->row_start && t->rows != (int64_t)t->B * t->max_rows) return SSD_ERR_SHAPE;
+  const int64_t tiles = ((int64_t)t->max_rows * (t->n_q_heads / cache->n_heads) + 15) / 16;
+  if ((int64_t)t->B * tiles * cache->n_heads > INT32_MAX) return SSD_ERR_SHAPE;
+  const int64_t hd = (int64_t)t->n_q_heads * cache->d_head;
+  if (t->ldq < hd || t->ldo < hd) return SSD_ERR_ARG;
+  cache_fields(cache, a);
+  a.B = t->B; a.rows = t->rows; a.max_rows = t->max_rows; a.max_len = t->max_len;
+  a.n_q_heads = t->n_q_heads; a.dtype = t->dtype; a.max_pages = t->max_pages;
+  return SSD_OK;
+}
+
 // The workspace of contexts made by ssd_create_static: one fixed array per device, resident from
 // the library's load until the process ends.  Host code never passes `scratch` itself to a
 // kernel or a copy (on the host it only names the symbol); it uses the device address that
@@ -1401,6 +1481,83 @@ int ssd_sync_status(ssd_ctx* c, int32_t* status) {
     if (hipMemset(c->at<int32_t>(c->L.status), 0, 4) != hipSuccess) return SSD_ERR_HIP;
     return SSD_ERR_DEVICE;
   }
+  return SSD_OK;
+}
+
+int ssd_page_map(int B, int page_size, int n_pages, int max_pages, const int32_t* d_seq_len,
+                 const int32_t* d_new, const int32_t* d_free, int n_free, int32_t* d_page_table,
+                 int32_t* d_row_start, int64_t* d_slot, int max_rows, int32_t* d_taken,
+                 int32_t* d_status, void* stream) {
+  if (!d_seq_len || !d_new || !d_page_table || !d_row_start || !d_taken || !d_status) return SSD_ERR_ARG;
+  if (n_free < 0 || max_rows < 0 || (n_free > 0 && !d_free) || (max_rows > 0 && !d_slot)) return SSD_ERR_ARG;
+  if (B < 1 || B > PAGE_MAP_MAX_BATCH || n_pages < 1 || !cache_pages_ok(page_size, max_pages)) return SSD_ERR_SHAPE;
+  PageMapArgs a;
+  a.B = B; a.page_size = page_size; a.n_pages = n_pages; a.max_pages = max_pages;
+  a.seq_len = d_seq_len; a.pos_off = 0; a.new_rows = d_new; a.new_const = 0;
+  a.free_pages = d_free; a.n_free = n_free; a.page_table = d_page_table;
+  a.row_start = d_row_start; a.slot = d_slot; a.max_rows = max_rows; a.taken = d_taken;
+  a.status = d_status;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  StreamDevice dev(s);
+  if (!dev.ok) return SSD_ERR_HIP;
+  HIP_TRY(launch_page_map(a, s));
+  return SSD_OK;
+}
+
+int ssd_cache_store(const ssd_cache* cache, int rows, const int64_t* d_slot, const void* d_k,
+                    const void* d_v, int64_t ld, int dtype, int32_t* d_status, void* stream) {
+  CacheRowsArgs a;
+  int rc = cache_rows(cache, rows, d_slot, d_k, d_v, ld, dtype, d_status, a);
+  if (rc || rows == 0) return rc;
+  a.k = d_k; a.v = d_v; a.k_out = a.v_out = nullptr;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  StreamDevice dev(s);
+  if (!dev.ok) return SSD_ERR_HIP;
+  HIP_TRY(launch_cache_store(a, s));
+  return SSD_OK;
+}
+
+int ssd_cache_load(const ssd_cache* cache, int rows, const int64_t* d_slot, void* d_k, void* d_v,
+                   int64_t ld, int dtype, int32_t* d_status, void* stream) {
+  CacheRowsArgs a;
+  int rc = cache_rows(cache, rows, d_slot, d_k, d_v, ld, dtype, d_status, a);
+  if (rc || rows == 0) return rc;
+  a.k = a.v = nullptr; a.k_out = d_k; a.v_out = d_v;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  StreamDevice dev(s);
+  if (!dev.ok) return SSD_ERR_HIP;
+  HIP_TRY(launch_cache_load(a, s));
+  return SSD_OK;
+}
+
+size_t ssd_cache_attention_workspace(const ssd_cache* cache, const ssd_cache_attn* attn) {
+  CacheAttnArgs a;
+  if (cache_attn_sizes(cache, attn, a)) return 0;
+  return cache_attn_part_floats(a) * sizeof(float);
+}
+
+int ssd_cache_attention(const ssd_cache* cache, const ssd_cache_attn* attn, void* d_workspace,
+                        size_t workspace_bytes, void* stream) {
+  CacheAttnArgs a;
+  int rc = cache_attn_sizes(cache, attn, a);
+  if (rc) return rc;
+  if (!cache_pointers_ok(cache) || !attn->seq_len || !attn->page_table || !attn->status) return SSD_ERR_ARG;
+  if (a.rows == 0) return SSD_OK;
+  const size_t elem = a.dtype == SSD_BF16 ? 2 : 4;
+  if (!attn->q || !attn->out || (uintptr_t)attn->q % elem || (uintptr_t)attn->out % elem) return SSD_ERR_ARG;
+  if (attn->bias ? attn->n_bias < 1 : attn->n_bias != 0) return SSD_ERR_ARG;
+  const size_t bytes = cache_attn_part_floats(a) * sizeof(float);
+  if (bytes && (!d_workspace || (uintptr_t)d_workspace % 256)) return SSD_ERR_ARG;
+  if (workspace_bytes < bytes) return SSD_ERR_CAPACITY;
+  a.q = attn->q; a.ldq = attn->ldq; a.out = attn->out; a.ldo = attn->ldo;
+  a.out_vec = (uintptr_t)a.out % (4 * elem) == 0 && ((size_t)a.ldo * elem) % (4 * elem) == 0;
+  a.row_start = attn->row_start; a.seq_len = attn->seq_len; a.pos_off = attn->pos_off;
+  a.page_table = attn->page_table; a.bias = attn->bias; a.n_bias = attn->n_bias;
+  a.scale = attn->scale; a.status = attn->status; a.part = reinterpret_cast<float*>(d_workspace);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  StreamDevice dev(s);
+  if (!dev.ok) return SSD_ERR_HIP;
+  HIP_TRY(launch_cache_attention(a, s));
   return SSD_OK;
 }
 

@@ -7,7 +7,7 @@ from __future__ import annotations
 
 import ctypes
 from dataclasses import dataclass
-from typing import Dict, Optional
+from typing import Dict, Optional, Sequence
 
 import numpy as np
 import torch
@@ -27,6 +27,147 @@ class Capacity:
     max_prompt: int
     page_size: int = 16
     spare_pages: int = 0  # pool pages beyond those the page table can reach at once
+
+
+class PagedCache:
+    """An 8-bit paged key/value cache on one device: int8 codes in pages with one scale for each
+    page and head (``ssd_cache``), a page table, and the pages not yet in use.
+
+    ``grow`` gives sequences new positions, ``append`` stores their rows, ``attend`` attends them
+    and ``rows`` reads them back.  All run on torch's current stream of the device.
+    """
+
+    def __init__(self, n_layers: int, n_heads: int, d_head: int, max_batch: int, max_seq: int,
+                 n_pages: int, page_size: int = 16, device: str = "cuda",
+                 page_seed: Optional[int] = None):
+        self.device = torch.device(device)
+        self.page_size, self.n_pages = page_size, n_pages
+        self.n_layers, self.n_heads, self.d_head = n_layers, n_heads, d_head
+        self.max_batch, self.max_pages = max_batch, (max_seq + page_size - 1) // page_size
+        shape = (n_layers, n_pages, n_heads, page_size, d_head)
+        self.k_codes = torch.zeros(shape, dtype=torch.int8, device=self.device)
+        self.v_codes = torch.zeros_like(self.k_codes)
+        self.k_scale = torch.zeros(shape[:3], dtype=torch.float32, device=self.device)
+        self.v_scale = torch.zeros_like(self.k_scale)
+        self.page_table = torch.full((max_batch, self.max_pages), -1, dtype=torch.int32,
+                                     device=self.device)
+        pages = np.arange(n_pages, dtype=np.int32)
+        if page_seed is not None:  # scatter sequences over the pool
+            pages = np.random.default_rng(page_seed).permutation(pages).astype(np.int32)
+        self.free = torch.from_numpy(pages).to(self.device)
+        self.used = 0                   # pages taken from the front of ``free``
+        self.lens = [0] * max_batch     # positions held, on the host and on the device
+        self.seq_len = torch.zeros(max_batch, dtype=torch.int32, device=self.device)
+        self.taken = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._workspace = torch.empty(0, dtype=torch.uint8, device=self.device)
+
+    def _stream(self) -> int:
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def _rows(self, t: torch.Tensor, heads: int, name: str) -> int:
+        """Row stride of t [rows, heads, d_head], whose rows are contiguous."""
+        if t.dim() != 3 or t.shape[1:] != (heads, self.d_head) or t.device != self.seq_len.device:
+            raise ValueError(f"{name}: [rows, {heads}, {self.d_head}] on {self.device} expected")
+        if t.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"{name}: float32 or bfloat16 expected")
+        if t.shape[0] and (t.stride(2) != 1 or t.stride(1) != self.d_head):
+            raise ValueError(f"{name}: the heads of a row must be contiguous")
+        return max(t.stride(0), heads * self.d_head) if t.shape[0] <= 1 else t.stride(0)
+
+    @staticmethod
+    def _dtype(t: torch.Tensor) -> int:
+        return abi.SSD_BF16 if t.dtype == torch.bfloat16 else abi.SSD_F32
+
+    def _layer(self, layer: int) -> abi.ssd_cache:
+        if not 0 <= layer < self.n_layers:
+            raise ValueError(f"layer {layer} of {self.n_layers}")
+        return abi.ssd_cache(self.k_codes[layer], self.v_codes[layer], self.k_scale[layer],
+                             self.v_scale[layer], self.n_pages, self.n_heads, self.page_size,
+                             self.d_head)
+
+    def grow(self, new: Sequence[int]):
+        """new[b] more positions for sequence b.  Returns (row_start [B + 1], slot [rows]): the
+        first row of each sequence among the new rows, and each row's slot."""
+        B, ps = len(new), self.page_size
+        if not 1 <= B <= self.max_batch or any(n < 0 for n in new):
+            raise ValueError("one non-negative count for each of at most max_batch sequences")
+        if any(l + n > self.max_pages * ps for l, n in zip(self.lens, new)):
+            raise ValueError("a sequence would be longer than the page table")
+        need = sum((l + n + ps - 1) // ps - (l + ps - 1) // ps for l, n in zip(self.lens, new))
+        if need > self.n_pages - self.used:
+            raise ValueError(f"{need} pages needed, {self.n_pages - self.used} free")
+        counts = torch.tensor(list(new), dtype=torch.int32, device=self.device)
+        row_start = torch.empty(B + 1, dtype=torch.int32, device=self.device)
+        slot = torch.empty(sum(new), dtype=torch.int64, device=self.device)
+        abi.ssd_page_map(B, ps, self.n_pages, self.max_pages, self.seq_len, counts,
+                         self.free[self.used:] if need else None, need, self.page_table, row_start,
+                         slot, sum(new), self.taken, self.status, self._stream())
+        self.used += need
+        for b, n in enumerate(new):
+            self.lens[b] += n
+        self.seq_len[:B] += counts
+        return row_start, slot
+
+    def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, slot: torch.Tensor) -> None:
+        """Store rows k, v [rows, heads, d_head] into the slots that ``grow`` returned."""
+        ld = self._rows(k, self.n_heads, "k")
+        if self._rows(v, self.n_heads, "v") != ld or v.shape != k.shape or v.dtype != k.dtype:
+            raise ValueError("k and v of one layout expected")
+        self._slots(slot, k.shape[0])
+        abi.ssd_cache_store(self._layer(layer), k.shape[0], slot, k, v, ld, self._dtype(k),
+                            self.status, self._stream())
+
+    def rows(self, layer: int, slot: torch.Tensor, dtype: torch.dtype = torch.float32):
+        """The values of cached rows: (k, v) [rows, heads, d_head]."""
+        k = torch.zeros(slot.numel(), self.n_heads, self.d_head, dtype=dtype, device=self.device)
+        v = torch.zeros_like(k)
+        ld = self._rows(k, self.n_heads, "dtype")
+        self._slots(slot, slot.numel())
+        abi.ssd_cache_load(self._layer(layer), slot.numel(), slot, k, v, ld, self._dtype(k),
+                           self.status, self._stream())
+        return k, v
+
+    def _slots(self, slot: torch.Tensor, rows: int) -> None:
+        if slot.dtype != torch.int64 or slot.shape != (rows,) or not slot.is_contiguous() or \
+                slot.device != self.seq_len.device:
+            raise ValueError(f"slot: int64 [{rows}] on {self.device} expected")
+
+    def attend(self, layer: int, q: torch.Tensor, row_start: torch.Tensor, max_rows: int,
+               scale: float, bias: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Causal attention of the last rows that ``grow`` gave: q [rows, query heads, d_head], the
+        rows of sequence b from row_start[b] on, at most max_rows of one.  bias [query heads, n] by
+        distance is added to the scores."""
+        heads = q.shape[1] if q.dim() == 3 else 0
+        ldq = self._rows(q, heads, "q")
+        B = row_start.numel() - 1
+        if row_start.dtype != torch.int32 or not row_start.is_contiguous() or \
+                not 1 <= B <= self.max_batch or row_start.device != self.seq_len.device:
+            raise ValueError("row_start: int32 [B + 1] expected")
+        if bias is not None and (bias.dtype != torch.float32 or bias.dim() != 2 or not bias.is_contiguous()
+                                 or bias.shape[0] != heads or bias.device != self.seq_len.device):
+            raise ValueError("bias: float32 [query heads, n] expected")
+        if out is None:
+            out = torch.zeros(q.shape, dtype=q.dtype, device=self.device)
+        ldo = self._rows(out, heads, "out")
+        if out.shape != q.shape or out.dtype != q.dtype:
+            raise ValueError("out: as q")
+        # the rows sit at the sequences' ends: before them, each holds its length less its rows
+        start = self.seq_len[:B] - (row_start[1:] - row_start[:-1])
+        a = abi.ssd_cache_attn(B=B, rows=q.shape[0], max_rows=max_rows,
+                               max_len=max(1, max(self.lens[:B])), n_q_heads=heads,
+                               dtype=self._dtype(q), q=q, ldq=ldq, out=out, ldo=ldo,
+                               row_start=row_start, seq_len=start, pos_off=0,
+                               max_pages=self.max_pages, page_table=self.page_table, bias=bias,
+                               n_bias=bias.shape[1] if bias is not None else 0, scale=scale,
+                               status=self.status)
+        cache = self._layer(layer)
+        nbytes = abi.ssd_cache_attention_workspace(cache, a)
+        if self._workspace.numel() < nbytes:
+            self._workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        abi.ssd_cache_attention(cache, a, self._workspace if nbytes else None, nbytes, self._stream())
+        return out
 
 
 class DeviceDecoder:

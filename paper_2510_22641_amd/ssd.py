@@ -18,7 +18,7 @@ SSD_OK, SSD_ERR_ARG, SSD_ERR_SHAPE, SSD_ERR_CAPACITY, SSD_ERR_HIP, SSD_ERR_STATE
 SSD_ARCH_T5, SSD_ARCH_LLAMA = 0, 1
 SSD_F32, SSD_BF16 = 0, 1
 SSD_MODE_GREEDY, SSD_MODE_SPECULATIVE, SSD_MODE_SPECULATIVE_DYNAMIC = 0, 1, 2
-SSD_DEV_BAD_TOKEN, SSD_DEV_CAPACITY, SSD_DEV_BAD_PAGE = 1, 2, 4
+SSD_DEV_BAD_TOKEN, SSD_DEV_CAPACITY, SSD_DEV_BAD_PAGE, SSD_DEV_NOT_FINITE = 1, 2, 4, 8
 
 
 class ssd_dims(ctypes.Structure):
@@ -48,6 +48,28 @@ class ssd_kv(ctypes.Structure):
     _fields_ = [("k_pool", c_void_p), ("v_pool", c_void_p), ("n_pages", c_int32),
                 ("page_table", c_void_p), ("seq_len", c_void_p), ("xk", c_void_p),
                 ("xv", c_void_p)]
+
+
+class _Described(ctypes.Structure):
+    """A descriptor whose pointer fields also take tensors, as the calls' arguments do."""
+
+    def __init__(self, *args, **kw):
+        kw.update(zip((n for n, _ in self._fields_), args))
+        pointers = {n for n, t in self._fields_ if t is c_void_p}
+        super().__init__(**{n: _p(v) if n in pointers else v for n, v in kw.items()})
+
+
+class ssd_cache(_Described):
+    _fields_ = [(n, c_void_p) for n in ("k_codes", "v_codes", "k_scale", "v_scale")] + \
+               [(n, c_int32) for n in ("n_pages", "n_heads", "page_size", "d_head")]
+
+
+class ssd_cache_attn(_Described):
+    _fields_ = [(n, c_int32) for n in ("B", "rows", "max_rows", "max_len", "n_q_heads", "dtype")] + \
+               [("q", c_void_p), ("ldq", c_int64), ("out", c_void_p), ("ldo", c_int64),
+                ("row_start", c_void_p), ("seq_len", c_void_p), ("pos_off", c_int32),
+                ("max_pages", c_int32), ("page_table", c_void_p), ("bias", c_void_p),
+                ("n_bias", c_int32), ("scale", c_float), ("status", c_void_p)]
 
 
 class SSDError(RuntimeError):
@@ -89,6 +111,13 @@ def _load():
         "ssd_profile_read": (c_int, [P, POINTER(c_int64), POINTER(ctypes.c_double),
                                      POINTER(ctypes.c_double)]),
         "ssd_read_bandwidth": (c_int, [P, c_size_t, P, c_int, P, POINTER(ctypes.c_double)]),
+        "ssd_page_map": (c_int, [c_int, c_int, c_int, c_int, P, P, P, c_int, P, P, P, c_int, P, P,
+                                 P]),
+        "ssd_cache_store": (c_int, [POINTER(ssd_cache), c_int, P, P, P, c_int64, c_int, P, P]),
+        "ssd_cache_load": (c_int, [POINTER(ssd_cache), c_int, P, P, P, c_int64, c_int, P, P]),
+        "ssd_cache_attention_workspace": (c_size_t, [POINTER(ssd_cache), POINTER(ssd_cache_attn)]),
+        "ssd_cache_attention": (c_int, [POINTER(ssd_cache), POINTER(ssd_cache_attn), P, c_size_t,
+                                        P]),
         "ssd_sync_status": (c_int, [P, POINTER(c_int32)]),
         "ssd_status_string": (ctypes.c_char_p, [c_int]),
         "ssd_destroy": (None, [P]),
@@ -105,7 +134,9 @@ EXPORTS = ("ssd_workspace_bytes", "ssd_create", "ssd_create_static", "ssd_prefil
            "ssd_accept", "ssd_draft_sample", "ssd_accept_sample", "ssd_generate", "ssd_draft_confident", "ssd_accept_counts",
            "ssd_generate_confident", "ssd_dynamic_gamma", "ssd_set_graphs", "ssd_set_hidden_export",
            "ssd_profile_enable",
-           "ssd_profile_read", "ssd_read_bandwidth", "ssd_sync_status",
+           "ssd_profile_read", "ssd_read_bandwidth", "ssd_page_map", "ssd_cache_store",
+           "ssd_cache_load", "ssd_cache_attention_workspace", "ssd_cache_attention",
+           "ssd_sync_status",
            "ssd_status_string", "ssd_destroy")
 
 
@@ -251,6 +282,35 @@ def ssd_read_bandwidth(d_buf, nbytes: int, d_out, reps: int, stream) -> float:
     _check("ssd_read_bandwidth", _lib.ssd_read_bandwidth(_p(d_buf), int(nbytes), _p(d_out),
                                                          int(reps), _p(stream), ctypes.byref(g)))
     return float(g.value)
+
+
+def ssd_page_map(B, page_size, n_pages, max_pages, d_seq_len, d_new, d_free, n_free, d_page_table,
+                 d_row_start, d_slot, max_rows, d_taken, d_status, stream):
+    _check("ssd_page_map", _lib.ssd_page_map(
+        B, page_size, n_pages, max_pages, _p(d_seq_len), _p(d_new), _p(d_free), n_free,
+        _p(d_page_table), _p(d_row_start), _p(d_slot), max_rows, _p(d_taken), _p(d_status),
+        _p(stream)))
+
+
+def ssd_cache_store(cache: ssd_cache, rows, d_slot, d_k, d_v, ld, dtype, d_status, stream):
+    _check("ssd_cache_store", _lib.ssd_cache_store(ctypes.byref(cache), rows, _p(d_slot), _p(d_k),
+                                                   _p(d_v), ld, dtype, _p(d_status), _p(stream)))
+
+
+def ssd_cache_load(cache: ssd_cache, rows, d_slot, d_k, d_v, ld, dtype, d_status, stream):
+    _check("ssd_cache_load", _lib.ssd_cache_load(ctypes.byref(cache), rows, _p(d_slot), _p(d_k),
+                                                 _p(d_v), ld, dtype, _p(d_status), _p(stream)))
+
+
+def ssd_cache_attention_workspace(cache: ssd_cache, attn: ssd_cache_attn) -> int:
+    return int(_lib.ssd_cache_attention_workspace(ctypes.byref(cache), ctypes.byref(attn)))
+
+
+def ssd_cache_attention(cache: ssd_cache, attn: ssd_cache_attn, d_workspace, workspace_bytes: int,
+                        stream):
+    _check("ssd_cache_attention", _lib.ssd_cache_attention(
+        ctypes.byref(cache), ctypes.byref(attn), _p(d_workspace), int(workspace_bytes),
+        _p(stream)))
 
 
 def ssd_sync_status(ctx):

@@ -1,0 +1,131 @@
+"""Refusals of the 8-bit paged cache's entry points: decided on the host, before any device call."""
+import ctypes
+import os
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+P = 4096  # stands for a device pointer: the calls below return before they use one
+
+
+@pytest.fixture(scope="module")
+def abi():
+    if not os.path.exists(os.path.join(ROOT, "paper_2510_22641_amd", "libssd.so")):
+        import __graft_entry__
+        __graft_entry__.build()
+    from paper_2510_22641_amd import ssd
+    return ssd
+
+
+def _code(fn, *args):
+    from paper_2510_22641_amd import ssd
+    with pytest.raises(ssd.SSDError) as e:
+        fn(*args)
+    return e.value.code
+
+
+def _cache(abi, **kw):
+    v = dict(k_codes=P, v_codes=P, k_scale=P, v_scale=P, n_pages=4, n_heads=2, page_size=16, d_head=64)
+    v.update(kw)
+    return abi.ssd_cache(**v)
+
+
+def test_page_map_refusals(abi):
+    ok = dict(B=2, page_size=16, n_pages=4, max_pages=4, d_seq_len=P, d_new=P, d_free=P, n_free=4,
+              d_page_table=P, d_row_start=P, d_slot=P, max_rows=8, d_taken=P, d_status=P, stream=None)
+    for bad, code in ((dict(d_seq_len=None), abi.SSD_ERR_ARG), (dict(d_new=None), abi.SSD_ERR_ARG),
+                      (dict(d_page_table=None), abi.SSD_ERR_ARG), (dict(d_row_start=None), abi.SSD_ERR_ARG),
+                      (dict(d_slot=None), abi.SSD_ERR_ARG), (dict(d_taken=None), abi.SSD_ERR_ARG),
+                      (dict(d_status=None), abi.SSD_ERR_ARG), (dict(d_free=None), abi.SSD_ERR_ARG),
+                      (dict(n_free=-1), abi.SSD_ERR_ARG), (dict(max_rows=-1), abi.SSD_ERR_ARG),
+                      (dict(B=0), abi.SSD_ERR_SHAPE), (dict(B=4097), abi.SSD_ERR_SHAPE),
+                      (dict(page_size=0), abi.SSD_ERR_SHAPE), (dict(page_size=257), abi.SSD_ERR_SHAPE),
+                      (dict(n_pages=0), abi.SSD_ERR_SHAPE), (dict(max_pages=0), abi.SSD_ERR_SHAPE),
+                      (dict(max_pages=(1 << 20) + 1), abi.SSD_ERR_SHAPE)):
+        assert _code(abi.ssd_page_map, *dict(ok, **bad).values()) == code, bad
+
+
+CACHE_BAD = (dict(k_codes=None), dict(v_codes=None), dict(k_scale=None), dict(v_scale=None),
+             dict(k_codes=P + 8), dict(v_scale=P + 2))
+SHAPE_BAD = (dict(n_pages=0), dict(n_heads=0), dict(page_size=0), dict(page_size=257), dict(d_head=96),
+             dict(d_head=32))
+
+
+@pytest.mark.parametrize("name", ["ssd_cache_store", "ssd_cache_load"])
+def test_row_refusals(abi, name):
+    fn = getattr(abi, name)
+    ok = dict(rows=3, slot=P, k=P, v=P, ld=128, dtype=abi.SSD_F32, status=P, stream=None)
+    for bad, code in ((dict(rows=-1), abi.SSD_ERR_ARG), (dict(rows=(1 << 24) + 1), abi.SSD_ERR_SHAPE),
+                      (dict(slot=None), abi.SSD_ERR_ARG), (dict(k=None), abi.SSD_ERR_ARG), (dict(v=None), abi.SSD_ERR_ARG),
+                      (dict(k=P + 2), abi.SSD_ERR_ARG), (dict(v=P + 1, dtype=abi.SSD_BF16), abi.SSD_ERR_ARG),
+                      (dict(ld=127), abi.SSD_ERR_ARG), (dict(dtype=2), abi.SSD_ERR_ARG), (dict(status=None), abi.SSD_ERR_ARG)):
+        assert _code(fn, _cache(abi), *dict(ok, **bad).values()) == code, bad
+    for bad in CACHE_BAD:
+        assert _code(fn, _cache(abi, **bad), *ok.values()) == abi.SSD_ERR_ARG, bad
+    for bad in SHAPE_BAD:
+        assert _code(fn, _cache(abi, **bad), *ok.values()) == abi.SSD_ERR_SHAPE, bad
+    fn(_cache(abi), *dict(ok, rows=0, slot=None, k=None, v=None).values())  # no rows: nothing to do
+    assert getattr(abi._lib, name)(None, 0, None, None, None, 0, 0, None, None) == abi.SSD_ERR_ARG
+
+
+def _attn(abi, **kw):
+    v = dict(B=2, rows=6, max_rows=3, max_len=50, n_q_heads=4, dtype=abi.SSD_F32, q=P, ldq=256, out=P, ldo=256,
+             seq_len=P, max_pages=4, page_table=P, scale=1.0, status=P)
+    v.update(kw)
+    return abi.ssd_cache_attn(**v)
+
+
+def test_attention_refusals(abi):
+    size = abi.ssd_cache_attention_workspace(_cache(abi), _attn(abi, max_len=5000))
+    assert size > 0
+    # a workspace is per row, head and key range: more rows need more, a short cache none
+    assert abi.ssd_cache_attention_workspace(_cache(abi), _attn(abi, max_len=64)) == 0
+    assert abi.ssd_cache_attention_workspace(_cache(abi), _attn(abi, B=0)) == 0
+
+    def code(at, cache=None, ws=P, n=size):
+        return _code(abi.ssd_cache_attention, cache or _cache(abi), at, ws, n, None)
+
+    for bad, want in ((dict(B=0), abi.SSD_ERR_SHAPE), (dict(B=4097), abi.SSD_ERR_SHAPE), (dict(rows=5), abi.SSD_ERR_SHAPE),
+                      (dict(rows=-1, row_start=P), abi.SSD_ERR_SHAPE), (dict(max_rows=0), abi.SSD_ERR_SHAPE),
+                      (dict(max_len=0), abi.SSD_ERR_SHAPE), (dict(n_q_heads=3), abi.SSD_ERR_SHAPE),
+                      (dict(n_q_heads=0), abi.SSD_ERR_SHAPE), (dict(dtype=2), abi.SSD_ERR_ARG), (dict(ldq=255), abi.SSD_ERR_ARG),
+                      (dict(ldo=255), abi.SSD_ERR_ARG), (dict(max_pages=0), abi.SSD_ERR_SHAPE),
+                      (dict(max_pages=1 << 21), abi.SSD_ERR_SHAPE), (dict(q=None), abi.SSD_ERR_ARG), (dict(out=None), abi.SSD_ERR_ARG),
+                      (dict(q=P + 2), abi.SSD_ERR_ARG), (dict(out=P + 1, dtype=abi.SSD_BF16), abi.SSD_ERR_ARG),
+                      (dict(seq_len=None), abi.SSD_ERR_ARG), (dict(page_table=None), abi.SSD_ERR_ARG),
+                      (dict(status=None), abi.SSD_ERR_ARG), (dict(bias=P), abi.SSD_ERR_ARG), (dict(n_bias=4), abi.SSD_ERR_ARG)):
+        assert code(_attn(abi, **bad)) == want, bad
+    for bad in CACHE_BAD:
+        assert code(_attn(abi), _cache(abi, **bad)) == abi.SSD_ERR_ARG, bad
+    for bad in SHAPE_BAD:
+        assert code(_attn(abi), _cache(abi, **bad)) == abi.SSD_ERR_SHAPE, bad
+    long = _attn(abi, max_len=5000)
+    assert code(long, ws=None) == abi.SSD_ERR_ARG
+    assert code(long, ws=P + 16) == abi.SSD_ERR_ARG
+    assert code(long, n=size - 1) == abi.SSD_ERR_CAPACITY
+    abi.ssd_cache_attention(_cache(abi), _attn(abi, rows=0, row_start=P), None, 0, None)  # no rows: nothing to do
+    assert abi._lib.ssd_cache_attention(None, ctypes.byref(long), None, 0, None) == abi.SSD_ERR_ARG
+    assert abi._lib.ssd_cache_attention(ctypes.byref(_cache(abi)), None, None, 0, None) == abi.SSD_ERR_ARG
+
+
+def test_paged_cache_refuses_what_its_pools_cannot_take():
+    import torch
+    from paper_2510_22641_amd import runtime
+    c = runtime.PagedCache(1, 2, 64, 2, 64, 5, device="cpu")
+    for new in ([], [1, 1, 1], [-1, 0], [65, 0], [64, 32]):
+        with pytest.raises(ValueError):
+            c.grow(new)
+    assert c.lens == [0, 0] and c.used == 0
+    x, slot = torch.zeros(3, 2, 64), torch.zeros(3, dtype=torch.int64)
+    for k, v, s in ((x[:, :1], x[:, :1], slot), (x.half(), x.half(), slot), (x, x.bfloat16(), slot), (x, x[:2], slot),
+                    (x.transpose(1, 2).contiguous().transpose(1, 2), x, slot), (x, x, slot.int()), (x, x, slot[:2]),
+                    (x, x, torch.zeros(6, dtype=torch.int64)[::2])):
+        with pytest.raises(ValueError):
+            c.append(0, k, v, s)
+    with pytest.raises(ValueError):
+        c.append(1, x, x, slot)
+    rs = torch.tensor([0, 1, 3], dtype=torch.int32)
+    for q, r, bias in ((x[..., :32], rs, None), (x, rs.long(), None), (x, torch.zeros(4, dtype=torch.int32), None),
+                       (x, rs, torch.zeros(3, 8)), (x, rs, torch.zeros(2, 8).double())):
+        with pytest.raises(ValueError):
+            c.attend(0, q, r, 2, 1.0, bias)
