@@ -21,6 +21,10 @@
  *   - Every pointer named d_* (and every pointer inside ssd_weights / ssd_kv) is device memory
  *     owned by the caller, which keeps it alive until the stream has finished the work.  The
  *     library allocates no device memory; it uses the caller's workspace (ssd_workspace_bytes).
+ *   - With an SSD_I8 cache each pass stores its keys and values as ssd_cache_store does, rows of a
+ *     pass on one page at once; the codes in a page that is filled over several passes are rounded
+ *     again where its scale rises, so they depend on how its rows came (a draft's first, then the
+ *     verify's).  An infinity or NaN among them sets SSD_DEV_NOT_FINITE.
  *   - Matrices are row-major [out][in] (y = W x).  Matrices, embeddings and visual tokens are
  *     in `wdtype`; norm gains, imitation-network biases and the relative-position bias table are
  *     float32.  KV pools are in `kvdtype`.
@@ -52,7 +56,7 @@ enum {
 };
 
 enum { SSD_ARCH_T5 = 0, SSD_ARCH_LLAMA = 1 };
-enum { SSD_F32 = 0, SSD_BF16 = 1 };
+enum { SSD_F32 = 0, SSD_BF16 = 1, SSD_I8 = 2 /* kvdtype only */ };
 enum {
   SSD_MODE_GREEDY = 0,
   SSD_MODE_SPECULATIVE = 1,
@@ -84,7 +88,8 @@ typedef struct {
   float norm_eps;       /* decoder RMSNorm eps (T5 1e-6, LLaMA 1e-5) */
   float ln_eps;         /* imitation-network LayerNorm eps (1e-5) */
   int32_t wdtype;       /* SSD_F32 or SSD_BF16: matrices, embeddings, visual tokens */
-  int32_t kvdtype;      /* SSD_F32 or SSD_BF16: KV pools and cross-attention K/V */
+  int32_t kvdtype;      /* SSD_F32 or SSD_BF16: KV pools and cross-attention K/V; SSD_I8: pools of
+                           int8 codes with scales (ssd_cache), cross-attention K/V float32 */
   int32_t draft_layers; /* k: the draft model is layers 1..k + imitation network + LM head */
   int32_t in_hidden;    /* imitation-network hidden width (multiple of 64) */
   int32_t in_residual;  /* 1: I(x) = x + FC2(GELU(FC1(LN(x)))); 0: FC2(GELU(FC1(LN(x)))) */
@@ -93,9 +98,9 @@ typedef struct {
   int32_t max_seq;      /* KV positions per sequence: prefix + prompt + T + max_gamma + 1; with the
                            stepwise calls on a batch whose sequences finish in different rounds,
                            max_gamma more (a finished sequence is still drafted and verified at
-                           its last length until the batch is done) */
+                           its last length until the batch is done).  At most 1024; SSD_I8: 65536 */
   int32_t max_prompt;   /* largest prompt length P passed to ssd_prefill */
-  int32_t page_size;    /* KV positions per page */
+  int32_t page_size;    /* KV positions per page (SSD_I8: at most 256) */
   int32_t max_pages;    /* page-table columns per sequence (>= ceil(max_seq / page_size)) */
 } ssd_dims;
 
@@ -133,13 +138,17 @@ typedef struct {
 
 /* The shared KV cache (device pointers, caller-owned). */
 typedef struct {
-  void* k_pool;              /* [L][n_pages][H][page_size][d_head] kvdtype */
+  void* k_pool;              /* [L][n_pages][H][page_size][d_head] kvdtype (SSD_I8: int8 codes,
+                                16-byte aligned) */
   void* v_pool;              /* same layout */
   int32_t n_pages;           /* pages per layer in the pools */
   const int32_t* page_table; /* [max_batch][max_pages]: page of positions [j*page_size, (j+1)*page_size) */
   int32_t* seq_len;          /* [max_batch]: valid positions; written only by prefill and accept */
-  void* xk;                  /* T5: [L][max_batch][H][n_visual][d_head] kvdtype, written by prefill */
+  void* xk;                  /* T5: [L][max_batch][H][n_visual][d_head] kvdtype (SSD_I8: float32),
+                                written by prefill */
   void* xv;                  /* T5: same */
+  float* k_scale;            /* SSD_I8: [L][n_pages][H], the scales of the blocks; else not read */
+  float* v_scale;            /* SSD_I8: same */
 } ssd_kv;
 
 typedef struct ssd_ctx ssd_ctx;

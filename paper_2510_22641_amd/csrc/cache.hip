@@ -60,7 +60,7 @@ __global__ __launch_bounds__(MAP_THREADS) void page_map_kernel(const PageMapArgs
   int* page0 = map_lds + a.B + 1;    // [B + 1] rank in the free list of its first new page
   __shared__ long long waves[MAP_THREADS / 64];
   const int tid = threadIdx.x;
-  const long long cap = (long long)a.max_pages * a.page_size;
+  const int cap = a.cap;
   int fault = 0;
   // pages of a sequence with `len` positions held and n new rows: [first, end) of its table row
   auto need = [&](int len, int n, int& first) {

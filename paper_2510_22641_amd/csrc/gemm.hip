@@ -400,7 +400,9 @@ __global__ __launch_bounds__(256, 2) void gemm_ring_kernel(const LinearArgs a) {
           atomicOr(a.status, cap ? SSD_DEV_CAPACITY : SSD_DEV_BAD_PAGE);
           continue;
         }
-        const size_t o = (((size_t)page * a.n_heads + hh) * a.kv.page_size + pos % a.kv.page_size) * a.d_head + d;
+        const size_t o = a.kvdtype == 2  // rows of the pass
+                             ? (size_t)m * a.n_per + c0 + 4 * g
+                             : (((size_t)page * a.n_heads + hh) * a.kv.page_size + pos % a.kv.page_size) * a.d_head + d;
         void* base = mat == 2 ? a.kv.v : a.kv.k;
         if (a.kvdtype == 1) {
           bf16_t* p = reinterpret_cast<bf16_t*>(base) + o;

@@ -162,7 +162,11 @@ __device__ __forceinline__ void qkv_store_pre(const LinearArgs& a, int mat, int 
     return;
   }
   const int slot = pos % a.kv.page_size;
-  if (a.kvdtype == 1) store_kv_pair<bf16_t>(a, p.page, slot, h, i, half, mat == 2, e0, e1);
+  if (a.kvdtype == 2) {  // rows of the pass
+    float* to = reinterpret_cast<float*>(mat == 2 ? a.kv.v : a.kv.k) + (size_t)row * a.n_per + c0;
+    to[0] = e0;
+    to[half] = e1;
+  } else if (a.kvdtype == 1) store_kv_pair<bf16_t>(a, p.page, slot, h, i, half, mat == 2, e0, e1);
   else store_kv_pair<float>(a, p.page, slot, h, i, half, mat == 2, e0, e1);
 }
 

@@ -17,7 +17,8 @@ enum Norm { NORM_NONE = 0, NORM_RMS = 1, NORM_LN = 2, NORM_SOFTMAX = 3 };
 
 // Paged KV addressing shared by the QKV epilogue and the attention kernels.
 struct PagedKV {
-  void* k;  // layer base of the pools [n_pages][H][page_size][dh]
+  void* k;  // layer base of the pools [n_pages][H][page_size][dh]; 8-bit caches: the pass's float32
+            // rows [M][H dh] on their way to the pools
   void* v;
   const int32_t* page_table;
   int max_pages;
@@ -79,7 +80,7 @@ struct LinearArgs {
   int ldl = 0;
   // EPI_QKV: row m = b*C + j sits at position kv.seq_len[b] + kv.pos_off + j
   PagedKV kv = {};
-  int C = 1, n_heads = 0, d_head = 0, kvdtype = 0, max_seq = 0;
+  int C = 1, n_heads = 0, d_head = 0, kvdtype = 0, max_seq = 0;  // kvdtype 2: kv.k and kv.v are rows
   const float* rope_cos = nullptr;  // [max_seq][d_head/2] or null (no rotation)
   const float* rope_sin = nullptr;
   int32_t* status = nullptr;        // SSD_DEV_CAPACITY / SSD_DEV_BAD_PAGE bits
@@ -378,6 +379,7 @@ struct PageMapArgs {
   int new_const;
   const int32_t* free_pages;  // [n_free], or null: the table has every page already
   int n_free;
+  int cap;                  // positions a sequence may hold, at most max_pages page_size
   int32_t* page_table;      // [B][max_pages]
   int32_t* row_start;       // [B + 1] or null
   int64_t* slot;            // [max_rows] or null

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <cstddef>
 #include <cstdint>
 #include <cstring>
 #include <map>
@@ -37,7 +38,7 @@ struct Layout {
       p_x, p_attn, p_ffn, p_inh, ssq, attn_part, fold_q, fold_o,
       bucket, rope_cos, rope_sin, status, cur_tok, g_pending, g_draft, g_target,
       g_count, g_active, g_nactive, g_stats, g_ndraft, g_drafting, g_draft_w, conf_lg,
-      fold_fg, kpart, wtab, total;
+      fold_fg, kpart, wtab, kv_rows, kv_slot, cache_part, total;
   int rows_max, head_rows, parts_max, ctx_max, plane_rows, attn_rows;
   int kpart_max = 0;  // K-range partials of the long row blocks' residual projections
   bool fold = false;  // the folded cross-attention matrices are carved (fold_q, fold_o)
@@ -71,6 +72,31 @@ bool fold_fg_ok(const ssd_dims& d) {
          d.d_ff >= d.d_model && d.d_model % 8 == 0 && HD % 8 == 0;
 }
 
+// An attention call over the 8-bit cache for C rows of B sequences (sizes only).
+CacheAttnArgs cache_attn_of(const ssd_dims& d, int B, int C) {
+  CacheAttnArgs a = {};
+  a.n_heads = a.n_q_heads = d.n_heads;
+  a.page_size = d.page_size;
+  a.d_head = d.d_head;
+  a.B = B; a.max_rows = C; a.rows = B * C; a.max_len = d.max_seq;
+  a.dtype = SSD_F32;
+  a.max_pages = d.max_pages;
+  return a;
+}
+
+// Most floats of partial results that a pass of this context's attention may need.
+size_t cache_part_max(const ssd_dims& d) {
+  const int C1 = d.max_gamma + 1 > ctx_len_max(d) ? d.max_gamma + 1 : ctx_len_max(d);
+  size_t most = 0;
+  for (int B = 1; B <= d.max_batch; ++B)
+    for (int C = 1; C <= C1; ++C) {
+      const size_t n = cache_attn_part_floats(cache_attn_of(d, B, C));
+      if (n == 0) break;  // more rows are split no further
+      if (n > most) most = n;
+    }
+  return most;
+}
+
 // Workspace layout: the scratch a chain of launches writes (residual rows, projections, operand
 // planes, argmax partials, the layer-k stash ...), the tables, the folded cross-attention and
 // the loop state of ssd_generate, each slice 256-byte aligned.  Without allow_fold the
@@ -97,10 +123,11 @@ bool make_layout(const ssd_dims& d, Layout& L, bool allow_fold = true, bool allo
   {
     const size_t R = rows, PR = bf16 ? (size_t)L.plane_rows : 0, head_rows = (size_t)L.head_rows;
     const size_t R1 = bf16 ? 1 : R;  // float32 rows of what the planes replace
+    const bool i8 = d.kvdtype == SSD_I8;
     L.x = take(R * D * 4);
     L.x1 = take((B * D + HD) * 4);  // room for a one-row attention output right after the row
     L.q = take(R * HD * 4);
-    L.attn = take(R1 * HD * 4);
+    L.attn = take((i8 ? R : R1) * HD * 4);
     L.ffn = take(R1 * (size_t)d.d_ff * 4);
     L.inh = take(B * (size_t)d.in_hidden * 4);
     L.xi = take(B * D * 4);
@@ -118,6 +145,10 @@ bool make_layout(const ssd_dims& d, Layout& L, bool allow_fold = true, bool allo
     // row blocks past 128 rows: room for four K-range partials of the residual projections
     L.kpart_max = bf16 && R > 128 ? 4 : 0;
     L.kpart = take((size_t)L.kpart_max * R * D * 4);
+    // 8-bit caches: a pass's keys and values in float32, their slots, the attention's partials
+    L.kv_rows = take(i8 ? 2 * R * HD * 4 : 0);
+    L.kv_slot = take(i8 ? R * 8 : 0);
+    L.cache_part = take(i8 ? cache_part_max(d) * 4 : 0);
   }
   L.vis = take(d.arch == SSD_ARCH_T5 ? B * (size_t)d.n_visual * D * 4 : 0);
   {
@@ -153,6 +184,12 @@ bool make_layout(const ssd_dims& d, Layout& L, bool allow_fold = true, bool allo
   return true;
 }
 
+// Positions of a sequence the 8-bit cache's kernels index: page arithmetic holds to 2^24.
+bool cache_pages_ok(int page_size, int max_pages) {
+  return page_size >= 1 && page_size <= CACHE_MAX_PAGE && max_pages >= 1 &&
+         (long long)max_pages * page_size <= 1 << 24;
+}
+
 bool dims_ok(const ssd_dims* d) {
   if (!d) return false;
   if (d->arch != SSD_ARCH_T5 && d->arch != SSD_ARCH_LLAMA) return false;
@@ -163,11 +200,14 @@ bool dims_ok(const ssd_dims* d) {
   if (d->in_hidden < 64 || d->in_hidden % 64) return false;
   if (d->draft_layers < 1 || d->draft_layers > d->n_layers) return false;
   if (d->wdtype != SSD_F32 && d->wdtype != SSD_BF16) return false;
-  if (d->kvdtype != SSD_F32 && d->kvdtype != SSD_BF16) return false;
+  const bool i8 = d->kvdtype == SSD_I8;
+  if (d->kvdtype != SSD_F32 && d->kvdtype != SSD_BF16 && !i8) return false;
   if (d->max_batch < 1 || d->max_batch > 256) return false;
   if (d->max_gamma < 0 || d->max_gamma > 32) return false;
   // (1024: the longest cache the attention kernels are tested with; their page arithmetic holds to 2^15)
-  if (d->max_seq < 2 || d->max_seq > 1024) return false;
+  // (8-bit caches: the length up to which the rotary and bias tables of a context are tested)
+  if (d->max_seq < 2 || d->max_seq > (i8 ? 65536 : 1024)) return false;
+  if (i8 && !cache_pages_ok(d->page_size, d->max_pages)) return false;
   if (d->max_prompt < 1 || d->page_size < 1 || d->max_pages < 1) return false;
   if ((long long)d->max_pages * d->page_size < d->max_seq) return false;
   if (ctx_len_max(*d) > d->max_seq) return false;
@@ -237,6 +277,8 @@ struct ssd_ctx {
   size_t xkv_layer_elems() const {
     return (size_t)d.max_batch * d.n_heads * d.n_visual * d.d_head;
   }
+  // type of the cross-attention keys and values, and of the pools that are not 8-bit
+  int xkvdtype() const { return d.kvdtype == SSD_BF16 ? SSD_BF16 : SSD_F32; }
   size_t kv_elem() const { return d.kvdtype == SSD_BF16 ? 2 : 4; }
   // device tables of pointers (Layout::wtab): 0 cross keys / values, 2 cross query, 3 cross output,
   // 4 cross norm gain, 5 W_o (entry 0 holds two pointers a layer)
@@ -259,8 +301,13 @@ namespace {
 
 PagedKV paged(ssd_ctx* c, int l, int pos_off) {
   PagedKV p;
-  p.k = (char*)c->kv.k_pool + (size_t)l * c->kv_layer_elems() * c->kv_elem();
-  p.v = (char*)c->kv.v_pool + (size_t)l * c->kv_layer_elems() * c->kv_elem();
+  if (c->d.kvdtype == SSD_I8) {
+    p.k = c->at<float>(c->L.kv_rows);
+    p.v = c->at<float>(c->L.kv_rows) + (size_t)c->L.rows_max * c->d.n_heads * c->d.d_head;
+  } else {
+    p.k = (char*)c->kv.k_pool + (size_t)l * c->kv_layer_elems() * c->kv_elem();
+    p.v = (char*)c->kv.v_pool + (size_t)l * c->kv_layer_elems() * c->kv_elem();
+  }
   p.page_table = c->kv.page_table;
   p.max_pages = c->d.max_pages;
   p.page_size = c->d.page_size;
@@ -304,6 +351,48 @@ LinearArgs lin(ssd_ctx* c) {
   return a;
 }
 
+// The slots of a pass's rows (8-bit caches; the same for every layer).
+int pass_slots(ssd_ctx* c, int B, int C, int pos_off) {
+  const ssd_dims& d = c->d;
+  PageMapArgs a = {};
+  a.B = B; a.page_size = d.page_size; a.n_pages = c->kv.n_pages; a.max_pages = d.max_pages;
+  a.seq_len = c->kv.seq_len; a.pos_off = pos_off; a.new_const = C; a.cap = d.max_seq;
+  a.page_table = const_cast<int32_t*>(c->kv.page_table);  // only read: no free pages are given
+  a.slot = c->at<int64_t>(c->L.kv_slot); a.max_rows = B * C;
+  a.status = c->at<int32_t>(c->L.status);
+  HIP_TRY(launch_page_map(a, c->stream));
+  return SSD_OK;
+}
+
+// Self-attention of a pass over an 8-bit cache: the projection's rows into the blocks, then the
+// queries over them.
+int attend_i8(ssd_ctx* c, int l, int B, int C, int pos_off, const float* q, float* out) {
+  const ssd_dims& d = c->d;
+  const bool t5 = d.arch == SSD_ARCH_T5;
+  const int HD = d.n_heads * d.d_head;
+  const PagedKV rows = paged(c, l, pos_off);
+  int8_t* k_codes = reinterpret_cast<int8_t*>(c->kv.k_pool) + (size_t)l * c->kv_layer_elems();
+  int8_t* v_codes = reinterpret_cast<int8_t*>(c->kv.v_pool) + (size_t)l * c->kv_layer_elems();
+  const size_t blocks = (size_t)c->kv.n_pages * d.n_heads;
+  CacheRowsArgs r = {};
+  r.k_codes = k_codes; r.v_codes = v_codes;
+  r.k_scale = c->kv.k_scale + l * blocks; r.v_scale = c->kv.v_scale + l * blocks;
+  r.n_pages = c->kv.n_pages; r.n_heads = d.n_heads; r.page_size = d.page_size; r.d_head = d.d_head;
+  r.rows = B * C; r.slot = c->at<int64_t>(c->L.kv_slot); r.k = rows.k; r.v = rows.v; r.ld = HD;
+  r.dtype = SSD_F32; r.status = c->at<int32_t>(c->L.status);
+  HIP_TRY(launch_cache_store(r, c->stream));
+  CacheAttnArgs a = cache_attn_of(d, B, C);
+  a.k_codes = k_codes; a.v_codes = v_codes; a.k_scale = r.k_scale; a.v_scale = r.v_scale;
+  a.n_pages = c->kv.n_pages;
+  a.q = q; a.ldq = HD; a.out = out; a.ldo = HD; a.out_vec = true;
+  a.seq_len = c->kv.seq_len; a.pos_off = pos_off; a.page_table = c->kv.page_table;
+  a.bias = t5 ? c->at<float>(c->L.bias_tab) : nullptr; a.n_bias = d.max_seq;
+  a.scale = t5 ? 1.0f : (float)(1.0 / std::sqrt((double)d.d_head));
+  a.status = r.status; a.part = c->at<float>(c->L.cache_part);
+  HIP_TRY(launch_cache_attention(a, c->stream));
+  return SSD_OK;
+}
+
 // Layers l0..l1-1 over rows r = b*C + j at positions seq_len[b] + pos_off + j.  When stash is set
 // the residual after layer stash_layer is also written to stash[b * ld_stash + ...].
 int run_layers(ssd_ctx* c, float* x, int B, int C, int pos_off, int l0, int l1, int stash_layer,
@@ -337,6 +426,11 @@ int run_layers(ssd_ctx* c, float* x, int B, int C, int pos_off, int l0, int l1, 
     if (!planes || !gain_next) return;
     a.out_planes = p_x; a.out_ssq = ssq; a.out_gain = gain_next;
   };
+  const bool i8 = d.kvdtype == SSD_I8;
+  if (i8 && l0 < l1) {
+    const int rc = pass_slots(c, B, C, pos_off);
+    if (rc) return rc;
+  }
   if (planes)
     HIP_TRY(launch_rows_prep(x, D, R, D, c->layers[l0].attn_norm, nullptr, 0.f, p_x, ssq, s));
   for (int l = l0; l < l1; ++l) {
@@ -365,7 +459,14 @@ int run_layers(ssd_ctx* c, float* x, int B, int C, int pos_off, int l0, int l1, 
     at.max_seq = d.max_seq; at.xk = at.xv = nullptr; at.n_keys = 0;
     at.scale = t5 ? 1.0f : (float)(1.0 / std::sqrt((double)d.d_head));
     at.status = status;
-    HIP_TRY(launch_attention(at, s));
+    if (i8) {
+      float* out = fg ? x + D : attn;
+      const int rc = attend_i8(c, l, B, C, pos_off, q, out);
+      if (rc) return rc;
+      if (planes) HIP_TRY(launch_rows_prep(out, HD, R, HD, nullptr, nullptr, 0.f, p_attn, nullptr, s));
+    } else {
+      HIP_TRY(launch_attention(at, s));
+    }
     if (fg) {
       // y = x + W_o o into the FFN buffer and the unnormalised scores fg . [x; o] in one launch,
       // then x = y + fold_o . softmax(scores / rms(y)) per head
@@ -437,6 +538,7 @@ int run_layers(ssd_ctx* c, float* x, int B, int C, int pos_off, int l0, int l1, 
       HIP_TRY(linear(a, p_x));
       AttnArgs xa = at;
       xa.cross = 1;
+      xa.kvdtype = c->xkvdtype();
       xa.bias = nullptr;
       xa.scale = 1.0f;
       xa.xk = (char*)c->kv.xk + (size_t)l * c->xkv_layer_elems() * c->kv_elem();
@@ -773,6 +875,9 @@ int check_create_args(const ssd_dims* dims, const ssd_weights* w, const ssd_kv* 
   if (!kv->k_pool || !kv->v_pool || !kv->page_table || !kv->seq_len || kv->n_pages < 1)
     return SSD_ERR_ARG;
   if (t5 && (!kv->xk || !kv->xv)) return SSD_ERR_ARG;
+  if (d.kvdtype == SSD_I8 &&
+      (!kv->k_scale || !kv->v_scale || (uintptr_t)kv->k_pool % 16 || (uintptr_t)kv->v_pool % 16))
+    return SSD_ERR_ARG;
   return SSD_OK;
 }
 
@@ -799,7 +904,8 @@ int init_ctx(ssd_ctx* c, const ssd_dims& d, const ssd_weights* w, const ssd_kv* 
   c->w = *w;
   for (int l = 0; l < d.n_layers; ++l) c->layers[l] = w->layers[l];
   c->w.layers = c->layers;
-  c->kv = *kv;
+  // (the scales are the descriptor's last fields: callers without an 8-bit cache may not have them)
+  std::memcpy(&c->kv, kv, d.kvdtype == SSD_I8 ? sizeof(*kv) : offsetof(ssd_kv, k_scale));
   c->stream = reinterpret_cast<hipStream_t>(stream);
   c->ws = ws;
   c->L = L;
@@ -858,12 +964,6 @@ struct StreamDevice {
     if (before >= 0) (void)hipSetDevice(before);
   }
 };
-
-// Positions of a sequence the 8-bit cache's kernels index: page arithmetic holds to 2^24.
-bool cache_pages_ok(int page_size, int max_pages) {
-  return page_size >= 1 && page_size <= CACHE_MAX_PAGE && max_pages >= 1 &&
-         (long long)max_pages * page_size <= 1 << 24;
-}
 
 bool cache_shape_ok(const ssd_cache* c) {
   return c->n_pages >= 1 && c->n_heads >= 1 && c->n_heads <= 4096 && c->page_size >= 1 &&
@@ -1060,7 +1160,7 @@ int ssd_prefill(ssd_ctx* c, int B, int P, const int32_t* d_prompt, const void* d
       a.M = MV; a.K = D; a.n_per = HD; a.epi = EPI_CROSS; a.in_planes = p_x;
       a.wtab = c->table(0); a.n_tab = 2 * d.n_layers;
       a.cross_k = c->kv.xk; a.cross_v = c->kv.xv; a.cross_batch = d.max_batch;
-      a.n_visual = d.n_visual; a.n_heads = d.n_heads; a.d_head = d.d_head; a.kvdtype = d.kvdtype;
+      a.n_visual = d.n_visual; a.n_heads = d.n_heads; a.d_head = d.d_head; a.kvdtype = c->xkvdtype();
       HIP_TRY(launch_linear_rows(a, s));
     } else {
       for (int l = 0; l < d.n_layers; ++l) {
@@ -1071,7 +1171,7 @@ int ssd_prefill(ssd_ctx* c, int B, int P, const int32_t* d_prompt, const void* d
           a.epi = EPI_STORE; a.y = tmp; a.ldy = HD;
           HIP_TRY(run_linear(c, a));
           void* dst = (char*)(which ? c->kv.xv : c->kv.xk) + (size_t)l * c->xkv_layer_elems() * c->kv_elem();
-          HIP_TRY(launch_scatter_cross(tmp, dst, B, d.n_visual, d.n_heads, d.d_head, d.kvdtype, s));
+          HIP_TRY(launch_scatter_cross(tmp, dst, B, d.n_visual, d.n_heads, d.d_head, c->xkvdtype(), s));
         }
       }
     }
@@ -1092,7 +1192,7 @@ int ssd_prefill(ssd_ctx* c, int B, int P, const int32_t* d_prompt, const void* d
       }
       HIP_TRY(hipEventRecord(c->ev_fork, s));
       HIP_TRY(hipStreamWaitEvent(c->side, c->ev_fork, 0));
-      HIP_TRY(launch_cross_fold(c->kv.xk, c->kv.xv, c->xkv_layer_elems(), d.kvdtype, c->table(2),
+      HIP_TRY(launch_cross_fold(c->kv.xk, c->kv.xv, c->xkv_layer_elems(), c->xkvdtype(), c->table(2),
                                 c->table(3), d.wdtype, d.n_layers, d.n_heads, d.n_visual, d.d_head, D,
                                 c->at<float>(c->L.fold_q), c->at<float>(c->L.fold_o), c->side));
       if (c->L.fg)
@@ -1495,6 +1595,7 @@ int ssd_page_map(int B, int page_size, int n_pages, int max_pages, const int32_t
   a.B = B; a.page_size = page_size; a.n_pages = n_pages; a.max_pages = max_pages;
   a.seq_len = d_seq_len; a.pos_off = 0; a.new_rows = d_new; a.new_const = 0;
   a.free_pages = d_free; a.n_free = n_free; a.page_table = d_page_table;
+  a.cap = max_pages * page_size;
   a.row_start = d_row_start; a.slot = d_slot; a.max_rows = max_rows; a.taken = d_taken;
   a.status = d_status;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);

@@ -193,6 +193,8 @@ class DeviceDecoder:
         # attention is unscaled and adds a unit-variance position bias); "bf16" is available
         kvd = kv_dtype or "f32"
         self.kvdtype = torch.bfloat16 if kvd == "bf16" else torch.float32
+        # "i8": codes with a scale for each page and head (PagedCache), a quarter of float32's bytes
+        self.i8 = kvd == "i8"
         self.page_seed = page_seed
         self.in_residual = shape.in_residual if in_residual is None else in_residual
         self.g: Dict[str, torch.Tensor] = {}
@@ -227,7 +229,8 @@ class DeviceDecoder:
         d.rel_buckets, d.rel_max_dist = sh.rel_buckets, sh.rel_max_dist
         d.rope_theta, d.norm_eps, d.ln_eps = sh.rope_theta, sh.norm_eps, sh.ln_eps
         d.wdtype = abi.SSD_BF16 if self.wdtype == torch.bfloat16 else abi.SSD_F32
-        d.kvdtype = abi.SSD_BF16 if self.kvdtype == torch.bfloat16 else abi.SSD_F32
+        d.kvdtype = abi.SSD_I8 if self.i8 else \
+            abi.SSD_BF16 if self.kvdtype == torch.bfloat16 else abi.SSD_F32
         d.draft_layers, d.in_hidden, d.in_residual = self.k, sh.in_width, int(self.in_residual)
         d.max_batch, d.max_gamma, d.max_seq = cap.max_batch, cap.max_gamma, cap.max_seq
         d.max_prompt, d.page_size = cap.max_prompt, cap.page_size
@@ -244,13 +247,20 @@ class DeviceDecoder:
         H, dh, L = sh.n_heads, sh.d_head, sh.n_layers
         n_table = cap.max_batch * dims.max_pages
         n_pages = n_table + cap.spare_pages
-        self.k_pool = torch.zeros((L, n_pages, H, cap.page_size, dh), dtype=self.kvdtype, device=dev)
-        self.v_pool = torch.zeros_like(self.k_pool)
-        pages = np.arange(n_pages, dtype=np.int32)
-        if self.page_seed is not None:  # scatter sequences over the pool to exercise the table
-            pages = np.random.default_rng(self.page_seed).permutation(pages).astype(np.int32)
-        pages = pages[:n_table]
-        self.page_table = torch.from_numpy(pages.reshape(cap.max_batch, dims.max_pages)).to(dev)
+        if self.i8:
+            self.cache = PagedCache(L, H, dh, cap.max_batch, dims.max_pages * cap.page_size, n_pages,
+                                    cap.page_size, device=dev, page_seed=self.page_seed)
+            self.cache.grow([dims.max_pages * cap.page_size] * cap.max_batch)
+            self.k_pool, self.v_pool = self.cache.k_codes, self.cache.v_codes
+            self.page_table = self.cache.page_table
+        else:
+            self.k_pool = torch.zeros((L, n_pages, H, cap.page_size, dh), dtype=self.kvdtype, device=dev)
+            self.v_pool = torch.zeros_like(self.k_pool)
+            pages = np.arange(n_pages, dtype=np.int32)
+            if self.page_seed is not None:  # scatter sequences over the pool to exercise the table
+                pages = np.random.default_rng(self.page_seed).permutation(pages).astype(np.int32)
+            pages = pages[:n_table]
+            self.page_table = torch.from_numpy(pages.reshape(cap.max_batch, dims.max_pages)).to(dev)
         self.seq_len = torch.zeros(cap.max_batch, dtype=torch.int32, device=dev)
         if sh.arch == "t5":
             self.xk = torch.zeros((L, cap.max_batch, H, sh.n_visual, dh), dtype=self.kvdtype, device=dev)
@@ -280,6 +290,9 @@ class DeviceDecoder:
         kv.page_table, kv.seq_len = self.page_table.data_ptr(), self.seq_len.data_ptr()
         kv.xk = self.xk.data_ptr() if self.xk is not None else None
         kv.xv = self.xv.data_ptr() if self.xv is not None else None
+        if self.i8:
+            kv.k_scale = self.cache.k_scale.data_ptr()
+            kv.v_scale = self.cache.v_scale.data_ptr()
         # a stream of its own (default priority): the null stream cannot be captured into graphs
         self.stream = torch.cuda.Stream(dev)
         torch.cuda.current_stream(dev).synchronize()

@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(HERE, "libssd.so")
 SSD_OK, SSD_ERR_ARG, SSD_ERR_SHAPE, SSD_ERR_CAPACITY, SSD_ERR_HIP, SSD_ERR_STATE, SSD_ERR_DEVICE = \
     0, -1, -2, -3, -4, -5, -6
 SSD_ARCH_T5, SSD_ARCH_LLAMA = 0, 1
-SSD_F32, SSD_BF16 = 0, 1
+SSD_F32, SSD_BF16, SSD_I8 = 0, 1, 2
 SSD_MODE_GREEDY, SSD_MODE_SPECULATIVE, SSD_MODE_SPECULATIVE_DYNAMIC = 0, 1, 2
 SSD_DEV_BAD_TOKEN, SSD_DEV_CAPACITY, SSD_DEV_BAD_PAGE, SSD_DEV_NOT_FINITE = 1, 2, 4, 8
 
@@ -47,7 +47,7 @@ class ssd_weights(ctypes.Structure):
 class ssd_kv(ctypes.Structure):
     _fields_ = [("k_pool", c_void_p), ("v_pool", c_void_p), ("n_pages", c_int32),
                 ("page_table", c_void_p), ("seq_len", c_void_p), ("xk", c_void_p),
-                ("xv", c_void_p)]
+                ("xv", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p)]
 
 
 class _Described(ctypes.Structure):

@@ -129,3 +129,25 @@ def test_paged_cache_refuses_what_its_pools_cannot_take():
                        (x, rs, torch.zeros(3, 8)), (x, rs, torch.zeros(2, 8).double())):
         with pytest.raises(ValueError):
             c.attend(0, q, r, 2, 1.0, bias)
+
+
+def test_contexts_with_an_8bit_cache(abi):
+    from tests.test_abi_cpu import _dims
+    i8 = abi.SSD_I8
+    assert abi.ssd_workspace_bytes(_dims(kvdtype=i8)) > 0
+    assert abi.ssd_workspace_bytes(_dims(kvdtype=i8, max_seq=4096, max_pages=256)) > 0
+    for bad in (dict(kvdtype=3), dict(kvdtype=i8, page_size=257), dict(kvdtype=i8, max_seq=65537, max_pages=5000),
+                dict(wdtype=i8), dict(max_seq=4096, max_pages=256)):
+        assert abi.ssd_workspace_bytes(_dims(**bad)) == 0, bad
+    layer = abi.ssd_layer_weights(*[P] * len(abi.LAYER_FIELDS))
+    layers = (abi.ssd_layer_weights * 4)(layer, layer, layer, layer)
+    w = abi.ssd_weights(*[P] * len(abi.GLOBAL_FIELDS), layers)
+    good = dict(k_pool=P, v_pool=P, n_pages=4, page_table=P, seq_len=P, xk=P, xv=P, k_scale=P, v_scale=P)
+    ctx = ctypes.c_void_p()
+    for bad in (dict(k_scale=None), dict(v_scale=None), dict(k_pool=P + 8), dict(v_pool=None)):
+        rc = abi._lib.ssd_create(ctypes.byref(_dims(kvdtype=i8)), ctypes.byref(w), ctypes.byref(abi.ssd_kv(**dict(good, **bad))),
+                                 256, 1 << 30, None, ctypes.byref(ctx))
+        assert rc == abi.SSD_ERR_ARG, bad
+    rc = abi._lib.ssd_create(ctypes.byref(_dims(kvdtype=i8)), ctypes.byref(w), ctypes.byref(abi.ssd_kv(**good)), 256, 1 << 10,
+                             None, ctypes.byref(ctx))
+    assert rc == abi.SSD_ERR_CAPACITY
