@@ -967,7 +967,8 @@ struct StreamDevice {
 
 bool cache_shape_ok(const ssd_cache* c) {
   return c->n_pages >= 1 && c->n_heads >= 1 && c->n_heads <= 4096 && c->page_size >= 1 &&
-         c->page_size <= CACHE_MAX_PAGE && (c->d_head == 64 || c->d_head == 128);
+         c->page_size <= CACHE_MAX_PAGE && (c->d_head == 64 || c->d_head == 128) &&
+         (uint64_t)c->n_pages * c->n_heads * c->page_size < UINT32_MAX;
 }
 
 bool cache_pointers_ok(const ssd_cache* c) {

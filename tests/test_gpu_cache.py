@@ -50,8 +50,10 @@ def attend_reference(c, layer, q, starts, counts, scale, bias=None):
     (d_head + 6) 2^-24 times sum |q k| scale + |bias|.  The exponential's argument is a difference of
     two scores times log2 e, its result one more rounding or two: in all e = 2 ds + (|d| + 6) 2^-24
     relative, d the difference, in the weights and again in their sum.  Sums over n keys in float32
-    add n 2^-24 each.  bf16 rows: the weights' two planes drop at most 2^-17, and the output is rounded
-    once (2^-8)."""
+    add n 2^-24 each.  Float32 queries and weights enter the products as two f16 planes, each within
+    2^-11 of what it rounds: 2^-22 in all, of sum |q k| scale and of the weights.  bf16 queries are
+    exact in one plane (8 bits in 11); their weights are one plane, within 2^-11, and the output is
+    rounded once (2^-8)."""
     H, G = c.n_heads, q.shape[1] // c.n_heads
     q64 = q.double().cpu()
     out, tol = torch.zeros_like(q64), torch.zeros_like(q64)
@@ -73,14 +75,14 @@ def attend_reference(c, layer, q, starts, counts, scale, bias=None):
             some = (x > -math.inf).any(1)
             top = torch.where(some, x.amax(1) if N else torch.zeros(n), 0.0)
             w = torch.exp(x - top[:, None])
-            ds = torch.where(x > -math.inf, (c.d_head + 6) * u * mag, 0.0).amax(1) if N else torch.zeros(n)
+            ds = torch.where(x > -math.inf, (c.d_head + 6 + 4) * u * mag, 0.0).amax(1) if N else torch.zeros(n)
             gap = torch.where(w > 1e-8, top[:, None] - x, 0.0).amax(1) if N else torch.zeros(n)
             L = w.sum(1)
             inv = torch.where(some, 1 / L, 0.0)[:, None]
             out[r:r + n, h] = w @ vh * inv
             e = 2 * ds + (gap + 6) * u
             near = (w @ vh.abs()) * inv
-            extra = 0.0 if q.dtype == F32 else 2.0 ** -17
+            extra = 2.0 ** (-22 if q.dtype == F32 else -11)
             tol[r:r + n, h] = near * (2 * e + 2 * (N + 8) * u + extra)[:, None] + 1e-30
         r += n
     if q.dtype == BF16:
