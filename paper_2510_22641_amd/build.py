@@ -23,7 +23,8 @@ LIB = os.path.join(HERE, "libssd.so")
 SOURCES = ["linear.hip", "gemv1.hip", "gemm.hip", "gemm_rows_bias.hip", "gemm_rows_store_rms.hip",
            "gemm_rows_resid.hip", "gemm_rows_qkv.hip", "gemm_rows_gated.hip",
            "gemm_rows_argmax.hip", "gemm_rows_cross.hip",
-           "attention.hip", "cache.hip", "cache_attention.hip", "misc.hip", "sample.hip", "ssd_api.hip"]
+           "attention.hip", "cache.hip", "cache_attention.hip",
+           "cache_attention_tile.hip", "misc.hip", "sample.hip", "ssd_api.hip"]
 ARCH = "gfx950"
 
 

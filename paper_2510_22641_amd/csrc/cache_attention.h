@@ -1,12 +1,14 @@
 // Device helpers shared by the kernels of attention over the 8-bit paged cache.
 //
-// Codes are whole numbers below 2^7, which f16 holds exactly, so the products run on the f16 matrix
-// instruction and the blocks' scales are applied to scores and weights.  Queries enter scaled by
-// a power of two that puts their row's largest element into [2^14, 2^15): bf16 ones as one f16
-// plane (11 bits against their 8), float32 ones as two (22 bits: an element is off by at most
-// 2^-23 of itself, less than a sum of 64 products in float32 loses).  Weights, scaled likewise, are
-// one plane for bf16 rows (2^-11, an eighth of the output's own rounding) and two for float32.
-// Below 2^-29 of a row's largest, where f16's exponents end, they are off by 2^-40 of it.
+// Codes are whole numbers below 2^7 and scales powers of two, so a code times the ratio of its scale
+// to the largest one of the keys it is worked on with is exact in f16 down to ratios of 2^-24, and
+// the products run on the f16 matrix instruction.  Queries enter scaled by a power of two that puts
+// their row's largest element into [2^14, 2^15): bf16 ones as one f16 plane (11 bits against
+// their 8), float32 ones as two (22 bits: an element is off by at most 2^-23 of itself, less than a
+// sum of 64 products in float32 loses).  Weights are one plane for bf16 rows (2^-11, an eighth of
+// the output's own rounding) and two for float32, W_TOP times their value: the reference that the
+// softmax subtracts follows the running maximum in steps of at least REF_STEP, so they stay under
+// 2^15, and those under 2^-21 of the reference's are off by 2^-32 of it.
 #pragma once
 
 #include "device.h"
@@ -21,7 +23,8 @@ typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr float W_TOP = 32768.f;  // weights' scale
+constexpr float W_TOP = 128.f;   // weights' scale
+constexpr float REF_STEP = 8.f;  // in powers of two
 
 template <typename T> struct Planes { static constexpr int N = sizeof(T) == 4 ? 2 : 1; };
 
@@ -34,34 +37,65 @@ __device__ __forceinline__ f16x8_t f16_frag(uint32_t a, uint32_t b, uint32_t c, 
   return __builtin_bit_cast(f16x8_t, make_uint4(a, b, c, d));
 }
 
-// Codes of dword w as f16: 0x64XX is 1024 + XX, from which 1152 leaves XX - 128, XX the code's
-// byte with its top bit flipped.
-__device__ __forceinline__ uint32_t code_pair(uint32_t w_flipped, uint32_t sel) {
-  const f16x2_t off = {(_Float16)-1152.f, (_Float16)-1152.f};
-  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, w_flipped, sel)) + off);
+// A pair of keys' scales over the largest, and what takes the codes' offset off again.
+struct Ratio {
+  f16x2_t r, off;
+};
+__device__ __forceinline__ Ratio ratio_of(float a, float b) {
+  Ratio t;
+  t.r = f16x2_t{(_Float16)a, (_Float16)b};
+  t.off = t.r * f16x2_t{(_Float16)-1152.f, (_Float16)-1152.f};
+  return t;
 }
 
-// Eight consecutive codes of a row.
-__device__ __forceinline__ f16x8_t codes8(uint32_t a, uint32_t b) {
+// Two bytes of dword w as f16 times their ratios: 0x64XX is 1024 + XX, so 1152 less leaves XX - 128,
+// XX the code's byte with its top bit flipped.
+__device__ __forceinline__ uint32_t code_pair(uint32_t w_flipped, uint32_t sel, const Ratio& t) {
+  const f16x2_t v = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, w_flipped, sel));
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(v, t.r, t.off));
+}
+
+// Eight consecutive codes of a key's row.
+__device__ __forceinline__ f16x8_t codes8(uint32_t a, uint32_t b, const Ratio& t) {
   a ^= 0x80808080u;
   b ^= 0x80808080u;
-  return f16_frag(code_pair(a, 0x04010400), code_pair(a, 0x04030402), code_pair(b, 0x04010400), code_pair(b, 0x04030402));
+  return f16_frag(code_pair(a, 0x04010400, t), code_pair(a, 0x04030402, t), code_pair(b, 0x04010400, t),
+                  code_pair(b, 0x04030402, t));
 }
 
-// Eight rows' dwords, four dimensions each: operand d is dimension d of the eight keys.
-__device__ __forceinline__ void columns4(const uint32_t (&w)[8], f16x8_t (&out)[4]) {
+// Eight keys' dwords, four dimensions each: operand d is dimension d of the eight keys.
+__device__ __forceinline__ void columns4(const uint32_t (&w)[8], const Ratio (&t)[4], f16x8_t (&out)[4]) {
   uint32_t p[4][4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const uint32_t a = w[2 * k] ^ 0x80808080u, b = w[2 * k + 1] ^ 0x80808080u;
     const uint32_t x = __builtin_amdgcn_perm(b, a, 0x05010400), y = __builtin_amdgcn_perm(b, a, 0x07030602);
-    p[0][k] = code_pair(x, 0x04010400);
-    p[1][k] = code_pair(x, 0x04030402);
-    p[2][k] = code_pair(y, 0x04010400);
-    p[3][k] = code_pair(y, 0x04030402);
+    p[0][k] = code_pair(x, 0x04010400, t[k]);
+    p[1][k] = code_pair(x, 0x04030402, t[k]);
+    p[2][k] = code_pair(y, 0x04010400, t[k]);
+    p[3][k] = code_pair(y, 0x04030402, t[k]);
   }
 #pragma unroll
   for (int d = 0; d < 4; ++d) out[d] = f16_frag(p[d][0], p[d][1], p[d][2], p[d][3]);
+}
+
+// A scale's power of two (0 where no block has been written), its exponent and its reciprocal (a
+// large number for 0, whose blocks' ratios are 0 all the same).
+__device__ __forceinline__ float pow2_of(float s) { return __uint_as_float(__float_as_uint(s) & 0x7f800000u); }
+__device__ __forceinline__ int exp_of(float p) { return (int)(__float_as_uint(p) >> 23) - 127; }
+__device__ __forceinline__ float pow2_inv(float p) { return __uint_as_float(0x7f000000u - __float_as_uint(p)); }
+
+// Factor of a unit's weights: W_TOP times its largest value scale over the largest so far, as an
+// exponent.  (Under 2^-60 the weights are nothing in f16; the bound keeps the sum's own scale finite.)
+__device__ __forceinline__ int weight_exp(float vtop, float vref) {
+  const int e = exp_of(W_TOP) + exp_of(vtop) - exp_of(vref);
+  return e < -60 ? -60 : e;
+}
+
+// The factor of a row's products over keys of largest key scale ktop.
+__device__ __forceinline__ float score_factor(float qf, float ktop) {
+  const float f = qf * ktop;
+  return f < FLT_MIN ? FLT_MIN : f;
 }
 
 // Eight floats as N f16 planes, each the rounding of what the one before leaves.
@@ -82,6 +116,12 @@ __device__ __forceinline__ void f16_planes(const float (&f)[8], f16x8_t (&out)[N
   }
 }
 
+// The largest of three, or NaN (one instruction: the other maximum would first bring each to
+// canonical form).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+
 // The maximum over the four lanes l % 16 + 16 g of a column.
 __device__ __forceinline__ float col_max(float v) {
   v = fmaxf(v, __shfl_xor(v, 16, SSD_WAVE));
@@ -92,32 +132,33 @@ __device__ __forceinline__ float col_sum(float v) {
   return v + __shfl_xor(v, 32, SSD_WAVE);
 }
 
-// The matrix operand of a query row: lane (row l % 16, g = l / 16) takes elements g DH / 4 + 8 t + i
-// of step t.  Returns what turns a product with it into a score over `scale`: 2^(e - 14), or NaN
-// where an element is not finite.
+// The matrix operand of a query row: lane (row l % 16, g = l / 16) takes elements 64 (t / 2) + 16 g +
+// 8 (t % 2) + i at step t, with the sign of `scale`.  Returns what turns a product with it into a
+// score: |scale| 2^(e - 14), positive, or NaN where an element is not finite.
 template <typename T, int DH>
-__device__ __forceinline__ float load_query(const T* row, int g, f16x8_t (&q)[DH / 32][Planes<T>::N]) {
+__device__ __forceinline__ float load_query(const T* row, int g, float scale, f16x8_t (&q)[DH / 32][Planes<T>::N]) {
   float f[DH / 32][8], top = 0.f;
   bool bad = false;
 #pragma unroll
   for (int t = 0; t < DH / 32; ++t)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float v = load_elem(row + g * (DH / 4) + 8 * t + i);
+      const float v = load_elem(row + 64 * (t / 2) + 16 * g + 8 * (t % 2) + i);
       f[t][i] = v;
       top = fmaxf(top, fabsf(v));
       bad |= !(fabsf(v) <= FLT_MAX);
     }
   top = col_max(bad ? INFINITY : top);
-  const int e = ilogbf(top);  // (INT_MAX or so where top is 0 or infinite: no use is made of it)
-  const bool fine = top <= FLT_MAX, some = top > 0.f && fine;
+  const bool fine = top <= FLT_MAX, some = top > 0.f && fine && scale != 0.f;
+  const int e = some ? ilogbf(top) : 0;
 #pragma unroll
   for (int t = 0; t < DH / 32; ++t) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[t][i] = some ? ldexpf(f[t][i], 14 - e) : 0.f;
+    for (int i = 0; i < 8; ++i) f[t][i] = some ? ldexpf(scale < 0.f ? -f[t][i] : f[t][i], 14 - e) : 0.f;
     f16_planes<Planes<T>::N>(f[t], q[t]);
   }
-  return fine ? (some ? ldexpf(1.f, e - 14) : 0.f) : NAN;
+  const float to = ldexpf(fabsf(scale), e - 14);
+  return !fine ? NAN : !some ? 1.f : to < FLT_MIN ? FLT_MIN : to;
 }
 
 // The rows of sequence b: first row and count, kept inside the buffers whatever row_start holds.
@@ -162,5 +203,26 @@ constexpr uint32_t NO_ROW = 0xffffffffu;
 __device__ __forceinline__ int page_of(int i, int page_size, uint32_t inv) {
   return page_size == 1 ? i : (int)__umulhi((uint32_t)i, inv);
 }
+
+// The running reference of a row's softmax.  Scores are t = s * f (+ bias); without a bias f carries
+// log2 e and t is in powers of two, with one t stays in natural units, where the type's lowest value
+// is a finite number (times log2 e it would not be).
+template <bool BIAS>
+struct Reference {
+  float ref = -INFINITY;  // subtracted from the scores; -inf before the first key
+
+  // Takes in the largest score of new keys (the same in the row's four lanes); whether any row of
+  // the wave moves, and then by what its sums shrink.
+  __device__ __forceinline__ bool move(float top, float& drop) {
+    constexpr float step = BIAS ? REF_STEP / LOG2E : REF_STEP;
+    drop = 1.f;
+    if (!__any(top > ref + step)) return false;  // (-inf + step is -inf)
+    const float next = fmaxf(ref, top);
+    drop = __builtin_amdgcn_exp2f((ref - (next == -INFINITY ? 0.f : next)) * (BIAS ? LOG2E : 1.f));
+    ref = next;
+    return true;
+  }
+  __device__ __forceinline__ float used() const { return ref == -INFINITY ? 0.f : ref; }  // weights of zero
+};
 
 }  // namespace ssd

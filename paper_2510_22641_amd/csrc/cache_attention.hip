@@ -4,6 +4,7 @@
 // 0 .. p of its pages; the scores are q . c s_k scale + bias[h][p - i] with c the key's codes and s_k
 // its block's scale, the output sum_i w_i s_v c_i over the softmax weights w.
 #include "cache_attention.h"
+#include <type_traits>
 
 namespace ssd {
 
@@ -13,34 +14,42 @@ constexpr int AW = 4;     // waves a block
 constexpr int UNIT = 32;  // keys a wave takes at once
 
 // What a wave needs of a unit before its products: codes as loaded, and scales.
-template <int DH>
+template <int DH, bool EVEN>
 struct Unit {
-  uint4 k[2][DH / 64];        // keys 16 h + lane % 16: DH / 4 codes from g DH / 4 on
+  uint4 k[2][DH / 64];        // keys 16 h + lane % 16: 16 codes from 64 i + 16 g on
   uint32_t v[DH / 64][8];     // keys 16 h + 4 g + e (8 = 4 h + e): DH / 16 codes from lane % 16 on
-  float ks, vs;               // of key lane % 32
-  uint32_t row;               // of key lane % 32
+  // EVEN: of the keys' halves, the same in every lane; else [0] of key lane % 32
+  float ks[EVEN ? 2 : 1], vs[EVEN ? 2 : 1];
+  uint32_t row[EVEN ? 2 : 1];
 };
 
-// NT times 16 (row, head) pairs of one sequence and cache head a block, one of `splits` ranges of
-// their keys.  Pair u of the sequence is row u / G, head hk G + u % G.  A wave takes units of 32 keys
-// straight from memory to matrix operands: lane (r = l % 16, g = l / 16) loads DH / 4 codes of keys
-// r and 16 + r, which are its rows of S^T = K Q^T (key order and the order of d are free as long as
-// both operands agree); the scores land with lane (pair l % 16, keys 4 g + e of either half), which
-// is again the operand layout of the weights in O^T = V^T P^T when its K index 8 g + i names key
+// Reads through the scalar unit, for addresses that are the same in every lane.
+template <typename V>
+__device__ __forceinline__ V scalar_load(const V* p) {
+  return *(const __attribute__((address_space(4))) V*)(uintptr_t)p;
+}
+
+// 16 (row, head) pairs of one sequence and cache head a block, one of `splits` ranges of their keys.
+// Pair u of the sequence is row u / G, head hk G + u % G.  A wave takes units of 32 keys straight from
+// memory to matrix operands: lane (r = l % 16, g = l / 16) loads 16 codes of each 64 of keys r and
+// 16 + r, which are its rows of S^T = K Q^T (key order and the order of d are free as long as both
+// operands agree); the scores land with lane (pair l % 16, keys 4 g + e of either half), which is
+// again the operand layout of the weights in O^T = V^T P^T when its K index 8 g + i names key
 // 4 g + i % 4 of half i / 4, so neither scores nor weights cross lanes but for the maximum.  V is
 // read row by row, DH / 16 codes a lane, and its bytes turned to columns in registers.  A unit's
-// codes and scales are requested one unit ahead of their use and its page-table entries two.  Each
-// wave keeps its own maximum, sum and reference scale; they meet in LDS once.
-// With a bias the scores stay in natural units, where the type's lowest value is a finite one (times
-// log2 e it would not be); without one they carry the log2 e of exp2.
+// codes and scales are requested one unit ahead of their use and its page-table entries two.  EVEN:
+// pages hold a multiple of 16 positions, so a half lies in one page and its entry and scales are
+// scalars; else every key has its own, which cross lanes.  Each wave keeps its own reference, sum
+// and largest value scale; they meet in LDS once.
 // Bound: bytes of codes for long contexts, the chain lengths -> table -> codes for short ones.
-template <typename T, int DH, bool BIAS, int NT>
-__global__ __launch_bounds__(64 * AW, NT == 1 ? 3 : 2) void cache_attn_kernel(const CacheAttnArgs a, const int tiles,
-                                                                              const int splits, const uint32_t ps_inv) {
+template <typename T, int DH, bool BIAS, bool EVEN>
+__global__ __launch_bounds__(64 * AW, DH == 64 ? 3 : 2) void cache_attn_kernel(const CacheAttnArgs a, const int tiles,
+                                                                               const int splits, const uint32_t ps_inv) {
   constexpr int KS = DH / 32;  // steps of 32 over d_head
   constexpr int NB = DH / 16;  // output blocks of 16 dimensions
   constexpr int VW = DH / 64;  // dwords of V a lane and key
   constexpr int NP = Planes<T>::N;
+  constexpr bool EXACT = BIAS || sizeof(T) == 4;  // weights from the scores' differences alone
   __shared__ float xo[AW][16][DH + 4];
   __shared__ float xm[AW][16], xl[AW][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -50,226 +59,263 @@ __global__ __launch_bounds__(64 * AW, NT == 1 ? 3 : 2) void cache_attn_kernel(co
   const int G = a.n_q_heads / a.n_heads;
   int r0, nr;
   seq_rows(a, b, r0, nr);
-  const int pairs = nr * G, u0 = tile * 16 * NT;
+  const int pairs = nr * G, u0 = tile * 16;
   if (u0 >= pairs) return;  // whole blocks
   const int base = a.seq_len[b] + a.pos_off;
   const int cap = a.max_pages * a.page_size;
-  const int first = base + u0 / G, last = base + min(u0 + 16 * NT - 1, pairs - 1) / G;  // rows of the block
+  const int first = base + u0 / G, last = base + min(u0 + 15, pairs - 1) / G;  // rows of the block
   if (last >= cap && tid == 0 && split == 0) atomicOr(a.status, SSD_DEV_CAPACITY);
   const int kend = min(last, cap - 1) + 1;
   const int units = kend > 0 ? (kend + UNIT - 1) / UNIT : 0;
-  const int per = (units + splits - 1) / splits;
+  // ranges of one length for all sequences, so that no block has more to do than another
+  int most = 0;
+  if (splits > 1) {
+    for (int i = lane; i < a.B; i += 64) most = max(most, a.seq_len[i]);
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) most = max(most, __shfl_xor(most, i, SSD_WAVE));
+    most = min(max(most + a.pos_off + a.max_rows, kend), cap);
+  }
+  const int per = splits > 1 ? ((most + UNIT - 1) / UNIT + splits - 1) / splits : units;
   const int x0 = split * per, x1 = min(x0 + per, units);
   const int32_t* table = a.page_table + (size_t)b * a.max_pages;
   bool bad_page = false;
 
-  // row of codes of key x 32 + lane % 32
-  auto entry = [&](int x) -> int {
-    const int key = x * UNIT + (lane & 31);
-    return x < x1 && key < kend ? table[page_of(key, a.page_size, ps_inv)] : -1;
-  };
-  auto row_of = [&](int x, int page) -> uint32_t {
-    const int key = x * UNIT + (lane & 31);
-    if (x >= x1 || key >= kend) return NO_ROW;
-    if (page < 0 || page >= a.n_pages) {
-      bad_page = true;
-      return NO_ROW;
+  const uint32_t k_off = n * DH + 16 * g, v_off = 4 * g * DH + n * (DH / 16);  // in a half of one page
+  constexpr int NE = EVEN ? 2 : 1;  // entries of a unit a lane holds
+  struct Entries { int page[NE]; };
+  auto entries = [&](int x) {
+    Entries t;
+#pragma unroll
+    for (int h = 0; h < NE; ++h) {
+      const int key = x * UNIT + (EVEN ? 16 * h : lane & 31);
+      t.page[h] = -1;
+      if (x < x1 && key < kend) {
+        const int32_t* p = table + page_of(key, a.page_size, ps_inv);
+        t.page[h] = EVEN ? scalar_load(p) : *p;
+      }
     }
-    return ((uint32_t)page * a.n_heads + hk) * a.page_size + (key - page_of(key, a.page_size, ps_inv) * a.page_size);
+    return t;
   };
-  auto request = [&](Unit<DH>& u, uint32_t row, int page) {
-    u.row = row;
-    u.ks = u.vs = 0.f;
-    if (row != NO_ROW) {
-      const size_t sc = (size_t)page * a.n_heads + hk;
-      u.ks = a.k_scale[sc];
-      u.vs = a.v_scale[sc];
+  auto request = [&](Unit<DH, EVEN>& u, int x, const Entries& t) {
+#pragma unroll
+    for (int h = 0; h < NE; ++h) {
+      const int key = x * UNIT + (EVEN ? 16 * h : lane & 31), page = t.page[h];
+      u.row[h] = NO_ROW;
+      u.ks[h] = u.vs[h] = 0.f;
+      if (x < x1 && key < kend) {
+        if (page < 0 || page >= a.n_pages) {
+          bad_page = true;
+        } else {
+          const size_t sc = (size_t)page * a.n_heads + hk;
+          u.ks[h] = EVEN ? scalar_load(a.k_scale + sc) : a.k_scale[sc];
+          u.vs[h] = EVEN ? scalar_load(a.v_scale + sc) : a.v_scale[sc];
+          u.row[h] = (uint32_t)sc * a.page_size + (key - page_of(key, a.page_size, ps_inv) * a.page_size);
+        }
+      }
     }
-    // keys without a row read the pools' first bytes: their scores are masked
+    // keys without a row read the pools' first rows: their scores are masked
+    if constexpr (EVEN) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t kr = __shfl(row, 16 * h + n, SSD_WAVE);
-      const uint4* p = reinterpret_cast<const uint4*>(a.k_codes + (size_t)(kr == NO_ROW ? 0 : kr) * DH + g * (DH / 4));
+      for (int h = 0; h < 2; ++h) {
+        const size_t at = (size_t)(u.row[h] == NO_ROW ? 0 : u.row[h]) * DH;
+        const int8_t* kb = a.k_codes + at;
+        const int8_t* vb = a.v_codes + at;
 #pragma unroll
-      for (int i = 0; i < DH / 64; ++i) u.k[h][i] = p[i];
+        for (int i = 0; i < DH / 64; ++i) u.k[h][i] = *reinterpret_cast<const uint4*>(kb + k_off + 64 * i);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t vr = __shfl(row, 16 * h + 4 * g + e, SSD_WAVE);
-        const uint32_t* pv = reinterpret_cast<const uint32_t*>(a.v_codes + (size_t)(vr == NO_ROW ? 0 : vr) * DH + n * (DH / 16));
+        for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int i = 0; i < VW; ++i) u.v[i][4 * h + e] = pv[i];
+          for (int i = 0; i < VW; ++i) u.v[i][4 * h + e] = *reinterpret_cast<const uint32_t*>(vb + v_off + e * DH + 4 * i);
+      }
+    } else {
+      auto at = [&](int key) -> size_t {
+        const uint32_t r = __shfl(u.row[0], key, SSD_WAVE);
+        return (size_t)(r == NO_ROW ? 0 : r) * DH;
+      };
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint4* pk = reinterpret_cast<const uint4*>(a.k_codes + at(16 * h + n) + 16 * g);
+#pragma unroll
+        for (int i = 0; i < DH / 64; ++i) u.k[h][i] = pk[4 * i];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t* pv = reinterpret_cast<const uint32_t*>(a.v_codes + at(16 * h + 4 * g + e) + n * (DH / 16));
+#pragma unroll
+          for (int i = 0; i < VW; ++i) u.v[i][4 * h + e] = pv[i];
+        }
       }
     }
   };
 
-  int pos[NT], hq[NT];
-  f16x8_t q[NT][KS][NP];
-  float qf[NT];
-  f32x4_t o[NT][NB];
-  float m[NT], l[NT];
   // (the first unit's entries before the queries: neither waits for the other)
-  int page1 = entry(x0 + wave);
+  Entries ahead = entries(x0 + wave);
+  const int ul = min(u0 + n, pairs - 1), jl = ul / G, hq = hk * G + (ul - jl * G), pos = base + jl;  // this lane's pair
+  f16x8_t q[KS][NP];
+  const float qf = load_query<T, DH>(reinterpret_cast<const T*>(a.q) + (size_t)(r0 + jl) * a.ldq + (size_t)hq * DH, g,
+                                     a.scale, q) * (BIAS ? 1.f : LOG2E);
+  const float* bias_row = BIAS ? a.bias + (size_t)hq * a.n_bias : nullptr;
+  Reference<BIAS> ref;
+  float l = 0.f, vref = 0.f;  // sum of the weights; largest value scale so far
+  f32x4_t o[NB];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int u = min(u0 + 16 * t + n, pairs - 1), j = u / G;
-    hq[t] = hk * G + (u - j * G);
-    pos[t] = base + j;
-    const T* qp = reinterpret_cast<const T*>(a.q) + (size_t)(r0 + j) * a.ldq + (size_t)hq[t] * DH;
-    qf[t] = load_query<T, DH>(qp, g, q[t]) * a.scale * (BIAS ? 1.f : LOG2E);
-    m[t] = -INFINITY;
-    l[t] = 0.f;
-#pragma unroll
-    for (int d = 0; d < NB; ++d) o[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  }
-  float vref = 0.f;  // weights are held over the largest value scale so far
-  Unit<DH> next;
-  request(next, row_of(x0 + wave, page1), page1);
-  page1 = entry(x0 + wave + AW);
+  for (int d = 0; d < NB; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  Unit<DH, EVEN> ua, ub;  // in turn: one in work, the other on its way
 
-  for (int x = x0 + wave; x < x1; x += AW) {
-    const Unit<DH> cur = next;
+  // Unit x from `cur`; the wave's next one on its way to `next`.
+  auto step = [&](const Unit<DH, EVEN>& cur, Unit<DH, EVEN>& next, int x) {
     if (x + AW < x1) {
-      request(next, row_of(x + AW, page1), page1);
-      page1 = entry(x + 2 * AW);
+      request(next, x + AW, ahead);
+      ahead = entries(x + 2 * AW);
     }
-    float bias[NT][8];
-    if (BIAS) {
+    const bool rows = EVEN ? cur.row[0] != NO_ROW && cur.row[NE - 1] != NO_ROW : __all(cur.row[0] != NO_ROW);
+    const bool full = rows && x * UNIT + UNIT - 1 <= first;  // no key of it is masked
+    float bias[8];
+    if constexpr (BIAS) {
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const float* bp = a.bias + (size_t)hq[t] * a.n_bias;
+      for (int i = 0; i < 8; ++i)
+        bias[i] = bias_row[max(0, min(pos - (x * UNIT + 16 * (i / 4) + 4 * g + i % 4), a.n_bias - 1))];
+    }
+    // scales over the unit's largest
+    float ktop = fmaxf(cur.ks[0], cur.ks[NE - 1]), vtop = fmaxf(cur.vs[0], cur.vs[NE - 1]);
+    if constexpr (!EVEN) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          bias[t][i] = bp[max(0, min(pos[t] - (x * UNIT + 16 * (i / 4) + 4 * g + i % 4), a.n_bias - 1))];
+      for (int i = 1; i < 32; i <<= 1) {
+        ktop = fmaxf(ktop, __shfl_xor(ktop, i, SSD_WAVE));
+        vtop = fmaxf(vtop, __shfl_xor(vtop, i, SSD_WAVE));
       }
     }
-    // weights are multiplied by vs W_TOP / vref
-    float vm = cur.vs;
-#pragma unroll
-    for (int s = 1; s < 32; s <<= 1) vm = fmaxf(vm, __shfl_xor(vm, s, SSD_WAVE));
-    const float vnew = fmaxf(vref, vm), vdrop = vnew > 0.f ? vref / vnew : 1.f;
-    const float vmul = vnew > 0.f ? cur.vs * (W_TOP / vnew) : cur.vs;
-    vref = vnew;
-    float ks[8], vs[8];
-    bool in[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int src = 16 * (i / 4) + 4 * g + i % 4;
-      ks[i] = __shfl(cur.ks, src, SSD_WAVE);
-      vs[i] = __shfl(vmul, src, SSD_WAVE);
-      in[i] = __shfl(cur.row, src, SSD_WAVE) != NO_ROW;
-    }
-    const bool all = __all(cur.row != NO_ROW) && x * UNIT + UNIT - 1 <= first;  // nothing to mask
-    f32x4_t s[NT][2];
+    ktop = pow2_of(ktop);
+    vtop = pow2_of(vtop);
+    const float kinv = pow2_inv(ktop), vinv = pow2_inv(vtop);
+    f32x4_t s[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-#pragma unroll
-      for (int t = 0; t < NT; ++t) s[t][h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      const float k = (EVEN ? cur.ks[h % NE] : __shfl(cur.ks[0], 16 * h + n, SSD_WAVE)) * kinv;
+      const Ratio kr = ratio_of(k, k);
+      s[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
       const uint32_t* kw = reinterpret_cast<const uint32_t*>(&cur.k[h][0]);
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
-        const f16x8_t kf = codes8(kw[2 * st], kw[2 * st + 1]);
+        const f16x8_t kf = codes8(kw[2 * st], kw[2 * st + 1], kr);
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int p = NP - 1; p >= 0; --p) s[t][h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[t][st][p], s[t][h], 0, 0, 0);
+        for (int p = NP - 1; p >= 0; --p) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[st][p], s[h], 0, 0, 0);
       }
     }
-    f16x8_t pf[NT][NP];
+    const float f = score_factor(qf, ktop);
+    if constexpr (BIAS) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      float w[8], mx = -INFINITY, sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        w[i] = s[t][i / 4][i % 4] * (ks[i] * qf[t]);
-        if (BIAS) w[i] += bias[t][i];
-        if (!all) w[i] = in[i] && x * UNIT + 16 * (i / 4) + 4 * g + i % 4 <= pos[t] ? w[i] : -INFINITY;
-        mx = fmaxf(mx, w[i]);
-      }
-      mx = fmaxf(m[t], col_max(mx));
-      const float mu = mx == -INFINITY ? 0.f : mx;  // rows without a key yet: weights of zero
-      const float al = __builtin_amdgcn_exp2f((m[t] - mu) * (BIAS ? LOG2E : 1.f));
-      m[t] = mx;
+      for (int i = 0; i < 8; ++i) s[i / 4][i % 4] = fmaf(s[i / 4][i % 4], f, bias[i]);
+    }
+    if (!full) {  // (uniform)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const bool none = w[i] == -INFINITY;
-        w[i] = __builtin_amdgcn_exp2f((w[i] - mu) * (BIAS ? LOG2E : 1.f));
-        sum += w[i];
-        w[i] *= vs[i];
-        if ((BIAS || !all) && none) w[i] = 0.f;
+        const int src = 16 * (i / 4) + 4 * g + i % 4;
+        const uint32_t row = EVEN ? cur.row[i / 4 % NE] : (uint32_t)__shfl(cur.row[0], src, SSD_WAVE);
+        if (row == NO_ROW || x * UNIT + src > pos) s[i / 4][i % 4] = -INFINITY;
       }
-      l[t] = l[t] * al + sum;
-      f16_planes<NP>(w, pf[t]);
-      const float drop = al * vdrop;
-      if (__any(drop != 1.f)) {
+    }
+    float mx = max3(max3(s[0][0], s[0][1], s[0][2]), max3(s[0][3], s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]));
+    mx = col_max(mx) * (BIAS ? 1.f : f);
+    float drop, vdrop = 1.f;
+    bool shrink = ref.move(mx, drop);
+    if (vtop > vref) {
+      vdrop = vref * vinv;
+      vref = vtop;
+      shrink = true;
+    }
+    if (shrink) {  // rare once a few units are seen
+      l *= drop;
 #pragma unroll
-        for (int d = 0; d < NB; ++d)
+      for (int d = 0; d < NB; ++d)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[t][d][e] *= drop;
-      }
+        for (int e = 0; e < 4; ++e) o[d][e] *= drop * vdrop;
+    }
+    const int we = weight_exp(vtop, vref);
+    const float mu = ref.used(), wf = ldexpf(1.f, we);
+    float w[8], sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float v = s[i / 4][i % 4];
+      if constexpr (BIAS) w[i] = __builtin_amdgcn_exp2f((v - mu) * LOG2E);
+      else w[i] = __builtin_amdgcn_exp2f(fmaf(v, f, (EXACT ? 0.f : (float)we) - mu));
+      sum += w[i];
+      if constexpr (EXACT) w[i] *= wf;
+    }
+    l += EXACT ? sum : ldexpf(sum, -we);
+    f16x8_t pf[NP];
+    f16_planes<NP>(w, pf);
+    Ratio vr[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {  // keys 2 k and 2 k + 1 of the lane's eight
+      const int src = 16 * (k / 2) + 4 * g + 2 * (k % 2);
+      if (EVEN) vr[k] = ratio_of(cur.vs[k / 2 % NE] * vinv, cur.vs[k / 2 % NE] * vinv);
+      else vr[k] = ratio_of(__shfl(cur.vs[0], src, SSD_WAVE) * vinv, __shfl(cur.vs[0], src + 1, SSD_WAVE) * vinv);
     }
 #pragma unroll
     for (int i = 0; i < VW; ++i) {
       f16x8_t vf[4];
-      columns4(cur.v[i], vf);
+      columns4(cur.v[i], vr, vf);
 #pragma unroll
       for (int d = 0; d < 4; ++d)
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int p = NP - 1; p >= 0; --p)
-            o[t][4 * i + d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[d], pf[t][p], o[t][4 * i + d], 0, 0, 0);
+        for (int p = NP - 1; p >= 0; --p)
+          o[4 * i + d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[d], pf[p], o[4 * i + d], 0, 0, 0);
+    }
+  };
+  if (x0 + wave < x1) {
+    request(ua, x0 + wave, ahead);
+    ahead = entries(x0 + wave + AW);
+    for (int x = x0 + wave; x < x1; x += 2 * AW) {
+      step(ua, ub, x);
+      if (x + AW < x1) step(ub, ua, x + AW);
     }
   }
   if (bad_page) atomicOr(a.status, SSD_DEV_BAD_PAGE);
   const float back = vref * (1.f / W_TOP);
+  l = col_sum(l);
+  // O^T block d, row 4 g + e: dimension NB (4 g + e) + d, so a lane holds DH / 4 consecutive ones
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    if (u0 + 16 * t >= pairs) break;  // whole blocks
-    if (t) __syncthreads();  // the previous tile's results are out
-    const float lt = col_sum(l[t]);
-    // O^T block d, row 4 g + e: dimension NB (4 g + e) + d, so a lane holds DH / 4 consecutive ones
+  for (int e = 0; e < 4; ++e)
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int d = 0; d < NB; d += 4)
+      *reinterpret_cast<float4*>(&xo[wave][n][NB * (4 * g + e) + d]) =
+          make_float4(o[d][e] * back, o[d + 1][e] * back, o[d + 2][e] * back, o[d + 3][e] * back);
+  if (g == 0) { xm[wave][n] = ref.ref; xl[wave][n] = l; }
+  __syncthreads();
+  // thread (pair, part): the waves' results
+  constexpr int PART = DH / 16;
+  const int pn = tid >> 4, d0 = (tid & 15) * PART;
+  const int pu = u0 + pn;
+  if (pu >= pairs) return;
+  float M = xm[0][pn];
 #pragma unroll
-      for (int d = 0; d < NB; d += 4)
-        *reinterpret_cast<float4*>(&xo[wave][n][NB * (4 * g + e) + d]) =
-            make_float4(o[t][d][e] * back, o[t][d + 1][e] * back, o[t][d + 2][e] * back, o[t][d + 3][e] * back);
-    if (g == 0) { xm[wave][n] = m[t]; xl[wave][n] = lt; }
-    __syncthreads();
-    // thread (pair, part): the waves' results
-    constexpr int PART = DH / 16;
-    const int pn = tid >> 4, d0 = (tid & 15) * PART;
-    const int pu = u0 + 16 * t + pn;
-    if (pu < pairs) {
-      float M = xm[0][pn];
+  for (int w = 1; w < AW; ++w) M = fmaxf(M, xm[w][pn]);
+  const float Mu = M == -INFINITY ? 0.f : M;
+  float L = 0.f, f[PART];
 #pragma unroll
-      for (int w = 1; w < AW; ++w) M = fmaxf(M, xm[w][pn]);
-      const float Mu = M == -INFINITY ? 0.f : M;
-      float L = 0.f, f[PART];
+  for (int i = 0; i < PART; ++i) f[i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < PART; ++i) f[i] = 0.f;
+  for (int w = 0; w < AW; ++w) {
+    const float c = __builtin_amdgcn_exp2f((xm[w][pn] - Mu) * (BIAS ? LOG2E : 1.f));
+    L += c * xl[w][pn];
 #pragma unroll
-      for (int w = 0; w < AW; ++w) {
-        const float c = __builtin_amdgcn_exp2f((xm[w][pn] - Mu) * (BIAS ? LOG2E : 1.f));
-        L += c * xl[w][pn];
-#pragma unroll
-        for (int i = 0; i < PART; ++i) f[i] += c * xo[w][pn][d0 + i];
-      }
-      const int pj = pu / G, ph = hk * G + (pu - pj * G);
-      const size_t row = (size_t)(r0 + pj);
-      if (splits > 1) {
-        float* p = a.part + (row * a.n_q_heads + ph) * splits * (DH + 2) + (size_t)split * DH + d0;
-        store_out<float, PART>(p, f, false);
-        float* ml = a.part + (row * a.n_q_heads + ph) * splits * (DH + 2) + (size_t)splits * DH + 2 * split;
-        if (d0 == 0) { ml[0] = M; ml[1] = L; }
-      } else {
-        const float inv = L == 0.f ? 0.f : 1.f / L;  // (NaN stays)
-#pragma unroll
-        for (int i = 0; i < PART; ++i) f[i] *= inv;
-        store_out<T, PART>(reinterpret_cast<T*>(a.out) + row * a.ldo + (size_t)ph * DH + d0, f, a.out_vec);
-      }
-    }
+    for (int i = 0; i < PART; ++i) f[i] += c * xo[w][pn][d0 + i];
   }
+  const int pj = pu / G, ph = hk * G + (pu - pj * G);
+  const size_t row = (size_t)(r0 + pj);
+  if (splits > 1) {
+    float* p = a.part + (row * a.n_q_heads + ph) * splits * (DH + 2);
+    store_out<float, PART>(p + (size_t)split * DH + d0, f, false);
+    if (d0 == 0) {
+      p[(size_t)splits * DH + 2 * split] = M;
+      p[(size_t)splits * DH + 2 * split + 1] = L;
+    }
+    return;
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;  // (NaN stays)
+#pragma unroll
+  for (int i = 0; i < PART; ++i) f[i] *= inv;
+  store_out<T, PART>(reinterpret_cast<T*>(a.out) + row * a.ldo + (size_t)ph * DH + d0, f, a.out_vec);
 }
 
 // The splits' results of row blockIdx.y of sequence blockIdx.z and one head: per pair `splits` rows
@@ -316,30 +362,44 @@ __global__ __launch_bounds__(MERGE) void cache_attn_merge_kernel(const CacheAttn
   }
 }
 
-// Tiles of 16 (row, head) pairs a block takes: two where a sequence has more than one, which halves
-// the reads and conversions of its keys.
-int tiles_of(const CacheAttnArgs& a) { return a.max_rows * (a.n_q_heads / a.n_heads) > 16 ? 2 : 1; }
+// (row, head) pairs of the longest sequence and cache head.
+long long pairs_of(const CacheAttnArgs& a) { return a.max_rows * (long long)(a.n_q_heads / a.n_heads); }
 
-long long blocks_of(const CacheAttnArgs& a, int nt) {
-  const long long pairs = a.max_rows * (long long)(a.n_q_heads / a.n_heads);
-  return a.B * ((pairs + 16 * nt - 1) / (16 * nt)) * a.n_heads;
+// Pairs a block takes.  16 in the kernel above.  Beyond, the kernel for many rows: 64 in four waves of
+// one tile each; 128 in eight of one tile; 256 in eight of two where that leaves a block for every
+// compute unit, since two tiles share what is read from LDS (4096 bf16 rows of 32 heads over 8192
+// positions: 455 us against 640), but not for float32 rows of 128, whose two tiles' operands do not
+// fit the registers (three times 608 rows: 104 us against 39).
+int block_pairs(const CacheAttnArgs& a) {
+  const long long p = pairs_of(a);
+  if (p <= 64) return p <= 16 ? 16 : 64;
+  const bool two = !(a.dtype == SSD_F32 && a.d_head == 128) && a.B * ((p + 255) / 256) * a.n_heads >= 256;
+  return two ? 256 : 128;
 }
 
-template <typename T, int DH, int NT>
-void launch_nt(const CacheAttnArgs& a, int splits, hipStream_t s) {
-  const int pairs = a.max_rows * (a.n_q_heads / a.n_heads), tiles = (pairs + 16 * NT - 1) / (16 * NT);
-  const dim3 grid((unsigned)blocks_of(a, NT), splits), block(64 * AW);
-  const uint32_t inv = (uint32_t)(((1ull << 32) + a.page_size - 1) / a.page_size);
-  if (a.bias) hipLaunchKernelGGL((cache_attn_kernel<T, DH, true, NT>), grid, block, 0, s, a, tiles, splits, inv);
-  else hipLaunchKernelGGL((cache_attn_kernel<T, DH, false, NT>), grid, block, 0, s, a, tiles, splits, inv);
+long long blocks_of(const CacheAttnArgs& a) {
+  const int n = block_pairs(a);
+  return a.B * ((pairs_of(a) + n - 1) / n) * a.n_heads;
 }
 
 template <typename T, int DH>
 hipError_t launch_t(const CacheAttnArgs& a, hipStream_t s) {
-  const int splits = cache_attn_splits(a);
-  if (tiles_of(a) == 2) launch_nt<T, DH, 2>(a, splits, s);
-  else launch_nt<T, DH, 1>(a, splits, s);
-  hipError_t e = hipGetLastError();
+  const int splits = cache_attn_splits(a), n = block_pairs(a);
+  hipError_t e;
+  if (n >= 64) {
+    e = launch_cache_attn_tile(a, n, splits, s);
+  } else {
+    const dim3 grid((unsigned)blocks_of(a), splits), block(64 * AW);
+    const int tiles = (int)((pairs_of(a) + 15) / 16);
+    const uint32_t inv = (uint32_t)(((1ull << 32) + a.page_size - 1) / a.page_size);
+#define LAUNCH(BIAS, EVEN) \
+  hipLaunchKernelGGL((cache_attn_kernel<T, DH, BIAS, EVEN>), grid, block, 0, s, a, tiles, splits, inv)
+    const bool even = a.page_size % 16 == 0;
+    if (a.bias) { if (even) LAUNCH(true, true); else LAUNCH(true, false); }
+    else { if (even) LAUNCH(false, true); else LAUNCH(false, false); }
+#undef LAUNCH
+    e = hipGetLastError();
+  }
   if (e != hipSuccess || splits == 1) return e;
   hipLaunchKernelGGL((cache_attn_merge_kernel<T, DH>), dim3(a.n_q_heads, a.max_rows, a.B), dim3(MERGE), 0, s, a, splits);
   return hipGetLastError();
@@ -347,11 +407,16 @@ hipError_t launch_t(const CacheAttnArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// Key ranges a (row, head) pair's keys are split into: enough blocks to give each compute unit
-// three, while a range keeps 128 keys (one unit a wave).
+// Key ranges a (row, head) pair's keys are split into: enough blocks to fill the 256 compute units,
+// while a range keeps 128 keys (one unit a wave).  Blocks of eight waves: one each.  Four waves: two
+// each (three of the few-row kernel with heads of 64, by their registers), but three for a batch in
+// the few-row kernel, whose ragged lengths leave some ranges empty (32 sequences of up to 4096
+// positions: 49 us against 54; one of 32768: 72 us against 60).
 int cache_attn_splits(const CacheAttnArgs& a) {
-  const long long blocks = blocks_of(a, tiles_of(a));
-  long long want = (3LL * 256 + blocks - 1) / blocks;
+  const long long blocks = blocks_of(a);
+  const int n = block_pairs(a);
+  const int per_cu = n >= 128 ? 1 : n == 16 && (a.d_head == 64 || a.B > 1) ? 3 : 2;
+  long long want = (256LL * per_cu + blocks - 1) / blocks;
   const long long most = (a.max_len + AW * UNIT - 1) / (AW * UNIT);
   if (want > most) want = most;
   if (want > CACHE_SPLITS_MAX) want = CACHE_SPLITS_MAX;
