@@ -156,24 +156,26 @@ __global__ __launch_bounds__(MAP_THREADS) void page_map_kernel(const PageMapArgs
   }
 }
 
-// Four consecutive elements of a row; VEC: the row is aligned for one load.
-template <typename T, bool VEC>
-__device__ __forceinline__ float4 load4(const T* p) {
-  if constexpr (!VEC) return make_float4(load_elem(p), load_elem(p + 1), load_elem(p + 2), load_elem(p + 3));
-  else if constexpr (sizeof(T) == 4) return *reinterpret_cast<const float4*>(p);
-  else {
-    const uint2 r = *reinterpret_cast<const uint2*>(p);
-    return make_float4(__uint_as_float(r.x << 16), __uint_as_float(r.x & 0xffff0000u),
-                       __uint_as_float(r.y << 16), __uint_as_float(r.y & 0xffff0000u));
+// Four consecutive elements of a row as they are stored; VEC: the row is aligned for one load.
+template <typename T> struct Raw4;
+template <> struct Raw4<float> {
+  float4 v;
+  __device__ __forceinline__ float4 values() const { return v; }
+};
+template <> struct Raw4<bf16_t> {
+  uint2 v;
+  __device__ __forceinline__ float4 values() const {
+    return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u),
+                       __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
   }
-}
-
-// |v| where it is finite, else 0; `bad` collects whether any was not.
-__device__ __forceinline__ float finite_abs(float v, bool& bad) {
-  const float m = fabsf(v);
-  if (m <= FLT_MAX) return m;
-  bad = true;
-  return 0.f;
+};
+template <typename T, bool VEC>
+__device__ __forceinline__ Raw4<T> load4(const T* p) {
+  Raw4<T> r;
+  if constexpr (VEC) r.v = *reinterpret_cast<const decltype(r.v)*>(p);
+  else if constexpr (sizeof(T) == 4) r.v = make_float4(p[0], p[1], p[2], p[3]);
+  else r.v = make_uint2(p[0] | (uint32_t)p[1] << 16, p[2] | (uint32_t)p[3] << 16);
+  return r;
 }
 
 // Exponent e >= -100 of the smallest scale 2^e with top <= 127 2^e (top >= 0, finite).
@@ -183,17 +185,45 @@ __device__ __forceinline__ int scale_exp(float top) {
   return e < -100 ? -100 : e;
 }
 
-// The code of x = v * 2^-e: nearest (even), an infinity the largest, a NaN zero.
-__device__ __forceinline__ uint32_t code_of(float x) {
-  const float r = fminf(fmaxf(rintf(x), -127.f), 127.f);
-  return (uint32_t)(int)(x == x ? r : 0.f) & 255u;
+// Codes of v / s, with inv = 1 / s: nearest (even).  For finite v, whose quotients are at most 127, the
+// sum with 1.5 2^23 rounds to a whole number and has it in its low bits.  ANY: an infinity gets the
+// largest code, a NaN zero.
+template <bool ANY>
+__device__ __forceinline__ uint32_t codes_of(const float4& v, float inv) {
+  auto code = [&](float x) -> uint32_t {
+    if (ANY) {
+      const float r = fminf(fmaxf(rintf(x * inv), -127.f), 127.f);
+      return (uint32_t)(int)(x == x ? r : 0.f);
+    }
+    return __float_as_uint(fmaf(x, inv, 12582912.f));
+  };
+  const uint32_t lo = __builtin_amdgcn_perm(code(v.y), code(v.x), 0x0c0c0400),
+                 hi = __builtin_amdgcn_perm(code(v.w), code(v.z), 0x04000c0c);
+  return lo | hi;
 }
 
-__device__ __forceinline__ uint32_t codes_of(const float4& v, float inv) {
-  return code_of(v.x * inv) | code_of(v.y * inv) << 8 | code_of(v.z * inv) << 16 | code_of(v.w * inv) << 24;
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+__device__ __forceinline__ uint32_t abs_bits(const float4& v, uint32_t top) {
+  return max(max(max(top, abs_bits(v.x)), max(abs_bits(v.y), abs_bits(v.z))), abs_bits(v.w));
+}
+__device__ __forceinline__ float finite_abs(const float4& v, float top) {
+  const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (fabsf(f[i]) <= FLT_MAX) top = fmaxf(top, fabsf(f[i]));
+  return top;
 }
 
 __device__ __forceinline__ float code_at(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
+
+// slot / page_size for slots below 2^40, ps_inv = 1 / page_size: the rounded product is within one
+// of the quotient.
+__device__ __forceinline__ int slot_page(int64_t s, int ps, double ps_inv) {
+  int q = (int)((double)s * ps_inv);
+  const int64_t r = s - (int64_t)q * ps;
+  q -= r < 0;
+  return q + (r >= ps);
+}
 
 constexpr int STORE_WAVES = 4;
 constexpr int STORE_HELD = 8;  // passes of rows kept in registers between the maximum and the codes
@@ -207,10 +237,13 @@ constexpr int STORE_HELD = 8;  // passes of rows kept in registers between the m
 // so nothing is atomic.  Bound: bytes for long prompts; the chain slot -> rows, codes and scale ->
 // reduction -> store for single tokens.
 template <typename T, int DH, bool VEC>
-__global__ __launch_bounds__(64 * STORE_WAVES) void cache_store_kernel(const CacheRowsArgs a, const int window) {
+__global__ __launch_bounds__(64 * STORE_WAVES) void cache_store_kernel(const CacheRowsArgs a, const int window,
+                                                                       const int groups, const double ps_inv) {
   constexpr int LPR = DH / 4, RPP = 64 / LPR;  // lanes a row, rows a pass
   const int lane = threadIdx.x & 63;
-  const int task = __builtin_amdgcn_readfirstlane(blockIdx.y * STORE_WAVES + (threadIdx.x >> 6));
+  // (neighbouring blocks on neighbouring heads: together they read whole rows)
+  const int w = blockIdx.x / groups;
+  const int task = __builtin_amdgcn_readfirstlane((blockIdx.x - w * groups) * STORE_WAVES + (threadIdx.x >> 6));
   if (task >= 2 * a.n_heads) return;  // whole waves
   const bool is_v = task >= a.n_heads;
   const int h = is_v ? task - a.n_heads : task;
@@ -221,17 +254,18 @@ __global__ __launch_bounds__(64 * STORE_WAVES) void cache_store_kernel(const Cac
   float* scales = is_v ? a.v_scale : a.k_scale;
   const int lr = lane / LPR, lc = (lane % LPR) * 4;
   // the stretches that begin in this window
-  const int w0 = blockIdx.x * window, w1 = min(w0 + window, a.rows);
+  const int w0 = w * window, w1 = min(w0 + window, a.rows);
   auto fits = [&](int64_t v) { return v >= 0 && v < n_slots; };
-  int64_t mine = -1;
+  const int64_t mine = w0 + lane < a.rows ? a.slot[w0 + lane] : -1;
+  const int64_t before = w0 > 0 ? a.slot[w0 - 1] : -1;
   bool first = false, back = false;
   {
     const int r = w0 + lane;
+    int64_t prev = __shfl_up(mine, 1, SSD_WAVE);
+    if (lane == 0) prev = before;
     if (r < w1) {
-      mine = a.slot[r];
-      const int64_t prev = r > 0 ? a.slot[r - 1] : -1;
       if (fits(mine)) {
-        first = r == 0 || (fits(prev) && prev / ps != mine / ps);
+        first = r == 0 || (fits(prev) && slot_page(prev, ps, ps_inv) != slot_page(mine, ps, ps_inv));
         back = r > 0 && !fits(prev);
       } else if (mine != -1 && task == 0) {
         atomicOr(a.status, SSD_DEV_BAD_PAGE);
@@ -242,13 +276,13 @@ __global__ __launch_bounds__(64 * STORE_WAVES) void cache_store_kernel(const Cac
   while (backs) {  // behind a row without a slot: the nearest row that has one decides
     const int at = __builtin_ctzll(backs);
     backs &= backs - 1;
-    const int64_t page = __shfl(mine, at, SSD_WAVE) / ps;
+    const int page = slot_page(__shfl(mine, at, SSD_WAVE), ps, ps_inv);
     bool own = true;
     for (int e = w0 + at - 2; e >= 0; e -= 64) {
       const int64_t v = e - lane >= 0 ? a.slot[e - lane] : -1;
       const uint64_t m = __ballot(fits(v));
       if (m) {
-        own = __shfl(v, __builtin_ctzll(m), SSD_WAVE) / ps != page;
+        own = slot_page(__shfl(v, __builtin_ctzll(m), SSD_WAVE), ps, ps_inv) != page;
         break;
       }
     }
@@ -263,7 +297,7 @@ __global__ __launch_bounds__(64 * STORE_WAVES) void cache_store_kernel(const Cac
       starts &= starts - 1;
       r0 = w0 + at;
       s0 = __shfl(mine, at, SSD_WAVE);
-      page = (int)(s0 / ps);
+      page = slot_page(s0, ps, ps_inv);
     }
     const int off = (int)(s0 - (int64_t)page * ps), run = r0;
     // rows of the run, up to the page's end, and the row with a slot that follows it
@@ -271,7 +305,8 @@ __global__ __launch_bounds__(64 * STORE_WAVES) void cache_store_kernel(const Cac
     int64_t next = -1;
     r0 = -1;
     for (int e = run; e < a.rows; e += 64) {
-      const int64_t v = e + lane < a.rows ? a.slot[e + lane] : -1;
+      int64_t v = mine;  // (the window's first run is looked at already)
+      if (e != w0) v = e + lane < a.rows ? a.slot[e + lane] : -1;
       const int i = e + lane - run;
       const uint64_t in = __ballot(i == n + lane && off + i < ps && v == s0 + i);
       const int k = ~in ? __builtin_ctzll(~in) : 64;
@@ -280,20 +315,25 @@ __global__ __launch_bounds__(64 * STORE_WAVES) void cache_store_kernel(const Cac
       if (more) {
         const int at = __builtin_ctzll(more);
         next = __shfl(v, at, SSD_WAVE);
-        if (next / ps == page) r0 = e + at;
+        if (slot_page(next, ps, ps_inv) == page) r0 = e + at;
         break;
       }
     }
     int8_t* block = codes + ((size_t)page * a.n_heads + h) * ps * DH;
     float* sp = scales + (size_t)page * a.n_heads + h;
     const float s_old = off ? *sp : 0.f;
-    float top = 0.f;
-    float4 kept[STORE_HELD];
+    // elements of the run's rows, counted from its first (VEC: ld < 2^20, so a byte count fits 32 bits)
+    const T* rows = src + (size_t)run * a.ld;
+    auto at = [&](int r) -> Raw4<T> {
+      if constexpr (VEC) return load4<T, VEC>(rows + (uint32_t)r * (uint32_t)a.ld);
+      else return load4<T, VEC>(rows + (size_t)r * a.ld);
+    };
+    Raw4<T> kept[STORE_HELD];
 #pragma unroll
     for (int p = 0; p < STORE_HELD; ++p) {
-      if (p * RPP < n) {  // uniform
+      if (p * RPP < n) {  // uniform; a row past the run repeats its last: no other maximum
         const int r = p * RPP + lr;
-        kept[p] = load4<T, VEC>(src + (size_t)(run + min(r, n - 1)) * a.ld);
+        kept[p] = at(min(r, n - 1));
       }
     }
     float held = 0.f;
@@ -302,39 +342,47 @@ __global__ __launch_bounds__(64 * STORE_WAVES) void cache_store_kernel(const Cac
 #pragma unroll
       for (int i = 0; i < 4; ++i) held = fmaxf(held, fabsf(code_at(w, i)));
     }
-    bool ignored = false;  // a stored scale that is not finite counts as zero
-    top = finite_abs(held * s_old, ignored);
+    held *= s_old;
+    if (!(held <= FLT_MAX)) held = 0.f;  // a stored scale that is not finite counts as zero
+    // largest magnitude as bits, which order as the numbers do
+    uint32_t top = __float_as_uint(held);
 #pragma unroll
-    for (int p = 0; p < STORE_HELD; ++p) {
-      if (p * RPP < n) {  // (a row past the run repeats its last: no other maximum)
-        top = fmaxf(fmaxf(top, finite_abs(kept[p].x, bad)), finite_abs(kept[p].y, bad));
-        top = fmaxf(fmaxf(top, finite_abs(kept[p].z, bad)), finite_abs(kept[p].w, bad));
-      }
+    for (int p = 0; p < STORE_HELD; ++p)
+      if (p * RPP < n) top = abs_bits(kept[p].values(), top);
+    for (int r = STORE_HELD * RPP + lr; r < n; r += RPP) top = abs_bits(at(r).values(), top);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, SSD_WAVE));
+    const bool any = top >= 0x7f800000u;  // uniform: something is not finite, and the finite ones count
+    if (any) {
+      bad = true;
+      float f = held;
+      for (int r = lr; r < n; r += RPP) f = finite_abs(at(r).values(), f);
+      top = __float_as_uint(wave_max(f));
     }
-    for (int r = STORE_HELD * RPP + lr; r < n; r += RPP) {
-      const float4 v = load4<T, VEC>(src + (size_t)(run + r) * a.ld);
-      top = fmaxf(fmaxf(top, finite_abs(v.x, bad)), finite_abs(v.y, bad));
-      top = fmaxf(fmaxf(top, finite_abs(v.z, bad)), finite_abs(v.w, bad));
-    }
-    const int e = scale_exp(wave_max(top));
+    const int e = scale_exp(__uint_as_float(top));
     const float s_new = __uint_as_float((uint32_t)(e + 127) << 23);
     const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
     if (off && s_new != s_old) {
       for (int r = lr; r < off; r += RPP) {
         uint32_t* p = reinterpret_cast<uint32_t*>(block + (size_t)r * DH + lc);
         const uint32_t w = *p;
-        *p = codes_of(make_float4(code_at(w, 0) * s_old, code_at(w, 1) * s_old, code_at(w, 2) * s_old,
-                                  code_at(w, 3) * s_old), inv);
+        *p = codes_of<true>(make_float4(code_at(w, 0) * s_old, code_at(w, 1) * s_old, code_at(w, 2) * s_old,
+                                        code_at(w, 3) * s_old), inv);
       }
     }
     uint32_t* dst = reinterpret_cast<uint32_t*>(block + (size_t)off * DH + lc);
+    if (any) {
+      for (int r = lr; r < n; r += RPP)
+        dst[r * LPR] = codes_of<true>(at(r).values(), inv);
+    } else {
 #pragma unroll
-    for (int p = 0; p < STORE_HELD; ++p) {
-      const int r = p * RPP + lr;
-      if (r < n) dst[(size_t)r * LPR] = codes_of(kept[p], inv);
+      for (int p = 0; p < STORE_HELD; ++p) {
+        const int r = p * RPP + lr;
+        if (r < n) dst[r * LPR] = codes_of<false>(kept[p].values(), inv);
+      }
+      for (int r = STORE_HELD * RPP + lr; r < n; r += RPP)
+        dst[r * LPR] = codes_of<false>(at(r).values(), inv);
     }
-    for (int r = STORE_HELD * RPP + lr; r < n; r += RPP)
-      dst[(size_t)r * LPR] = codes_of(load4<T, VEC>(src + (size_t)(run + r) * a.ld), inv);
     if (lane == 0) *sp = s_new;
     if (r0 >= 0) {  // another run on this page, which reads what was just written
       s0 = next;
@@ -388,15 +436,17 @@ bool aligned(const void* p, int64_t ld, size_t elem, size_t bytes) {
 }
 
 template <typename T>
-hipError_t store_t(const CacheRowsArgs& a, int window, dim3 grid, hipStream_t s) {
-  const bool vec = aligned(a.k, a.ld, sizeof(T), 4 * sizeof(T)) && aligned(a.v, a.ld, sizeof(T), 4 * sizeof(T));
+hipError_t store_t(const CacheRowsArgs& a, int window, int groups, dim3 grid, hipStream_t s) {
+  const double ps_inv = 1.0 / a.page_size;
+  const bool vec = aligned(a.k, a.ld, sizeof(T), 4 * sizeof(T)) && aligned(a.v, a.ld, sizeof(T), 4 * sizeof(T)) &&
+                   a.ld < 1 << 20;
   const dim3 block(64 * STORE_WAVES);
   if (a.d_head == 64) {
-    if (vec) hipLaunchKernelGGL((cache_store_kernel<T, 64, true>), grid, block, 0, s, a, window);
-    else hipLaunchKernelGGL((cache_store_kernel<T, 64, false>), grid, block, 0, s, a, window);
+    if (vec) hipLaunchKernelGGL((cache_store_kernel<T, 64, true>), grid, block, 0, s, a, window, groups, ps_inv);
+    else hipLaunchKernelGGL((cache_store_kernel<T, 64, false>), grid, block, 0, s, a, window, groups, ps_inv);
   } else {
-    if (vec) hipLaunchKernelGGL((cache_store_kernel<T, 128, true>), grid, block, 0, s, a, window);
-    else hipLaunchKernelGGL((cache_store_kernel<T, 128, false>), grid, block, 0, s, a, window);
+    if (vec) hipLaunchKernelGGL((cache_store_kernel<T, 128, true>), grid, block, 0, s, a, window, groups, ps_inv);
+    else hipLaunchKernelGGL((cache_store_kernel<T, 128, false>), grid, block, 0, s, a, window, groups, ps_inv);
   }
   return hipGetLastError();
 }
@@ -415,8 +465,9 @@ hipError_t launch_cache_store(const CacheRowsArgs& a, hipStream_t s) {
   // One row a wave while that leaves the device room; long prompts 16, a usual page's worth, since
   // most waves of one row would find that their row begins no run.
   const int window = a.rows > 256 ? 16 : 1;
-  const dim3 grid((a.rows + window - 1) / window, (2 * a.n_heads + STORE_WAVES - 1) / STORE_WAVES);
-  return a.dtype == 1 ? store_t<bf16_t>(a, window, grid, s) : store_t<float>(a, window, grid, s);
+  const int groups = (2 * a.n_heads + STORE_WAVES - 1) / STORE_WAVES;
+  const dim3 grid((unsigned)((a.rows + window - 1) / window) * groups);
+  return a.dtype == 1 ? store_t<bf16_t>(a, window, groups, grid, s) : store_t<float>(a, window, groups, grid, s);
 }
 
 hipError_t launch_cache_load(const CacheRowsArgs& a, hipStream_t s) {

@@ -37,7 +37,7 @@ __device__ __forceinline__ V scalar_load(const V* p) {
 // again the operand layout of the weights in O^T = V^T P^T when its K index 8 g + i names key
 // 4 g + i % 4 of half i / 4, so neither scores nor weights cross lanes but for the maximum.  V is
 // read row by row, DH / 16 codes a lane, and its bytes turned to columns in registers.  A unit's
-// codes and scales are requested one unit ahead of their use and its page-table entries two.  EVEN:
+// codes and scales are requested two units ahead of their use and its page-table entries three.  EVEN:
 // pages hold a multiple of 16 positions, so a half lies in one page and its entry and scales are
 // scalars; else every key has its own, which cross lanes.  Each wave keeps its own reference, sum
 // and largest value scale; they meet in LDS once.
@@ -73,7 +73,8 @@ __global__ __launch_bounds__(64 * AW, DH == 64 ? 3 : 2) void cache_attn_kernel(c
     for (int i = lane; i < a.B; i += 64) most = max(most, a.seq_len[i]);
 #pragma unroll
     for (int i = 1; i < 64; i <<= 1) most = max(most, __shfl_xor(most, i, SSD_WAVE));
-    most = min(max(most + a.pos_off + a.max_rows, kend), cap);
+    // (one value in all lanes; known to be, so that what follows from it stays scalar)
+    most = __builtin_amdgcn_readfirstlane(min(max(most + a.pos_off + a.max_rows, kend), cap));
   }
   const int per = splits > 1 ? ((most + UNIT - 1) / UNIT + splits - 1) / splits : units;
   const int x0 = split * per, x1 = min(x0 + per, units);
@@ -83,16 +84,15 @@ __global__ __launch_bounds__(64 * AW, DH == 64 ? 3 : 2) void cache_attn_kernel(c
   const uint32_t k_off = n * DH + 16 * g, v_off = 4 * g * DH + n * (DH / 16);  // in a half of one page
   constexpr int NE = EVEN ? 2 : 1;  // entries of a unit a lane holds
   struct Entries { int page[NE]; };
+  // (No load depends on a branch, here and in `request`: the counts by which a wave waits for its
+  // loads stay known, and it waits for no later one.)
   auto entries = [&](int x) {
     Entries t;
 #pragma unroll
     for (int h = 0; h < NE; ++h) {
-      const int key = x * UNIT + (EVEN ? 16 * h : lane & 31);
-      t.page[h] = -1;
-      if (x < x1 && key < kend) {
-        const int32_t* p = table + page_of(key, a.page_size, ps_inv);
-        t.page[h] = EVEN ? scalar_load(p) : *p;
-      }
+      const int key = min(x * UNIT + (EVEN ? 16 * h : lane & 31), kend - 1);
+      const int32_t* p = table + page_of(key, a.page_size, ps_inv);
+      t.page[h] = EVEN ? scalar_load(p) : *p;
     }
     return t;
   };
@@ -100,18 +100,12 @@ __global__ __launch_bounds__(64 * AW, DH == 64 ? 3 : 2) void cache_attn_kernel(c
 #pragma unroll
     for (int h = 0; h < NE; ++h) {
       const int key = x * UNIT + (EVEN ? 16 * h : lane & 31), page = t.page[h];
-      u.row[h] = NO_ROW;
-      u.ks[h] = u.vs[h] = 0.f;
-      if (x < x1 && key < kend) {
-        if (page < 0 || page >= a.n_pages) {
-          bad_page = true;
-        } else {
-          const size_t sc = (size_t)page * a.n_heads + hk;
-          u.ks[h] = EVEN ? scalar_load(a.k_scale + sc) : a.k_scale[sc];
-          u.vs[h] = EVEN ? scalar_load(a.v_scale + sc) : a.v_scale[sc];
-          u.row[h] = (uint32_t)sc * a.page_size + (key - page_of(key, a.page_size, ps_inv) * a.page_size);
-        }
-      }
+      const bool in = x < x1 && key < kend, ok = in && page >= 0 && page < a.n_pages;
+      bad_page |= in && !ok;
+      const size_t sc = (size_t)(ok ? page : 0) * a.n_heads + hk;
+      u.ks[h] = EVEN ? scalar_load(a.k_scale + sc) : a.k_scale[sc];
+      u.vs[h] = EVEN ? scalar_load(a.v_scale + sc) : a.v_scale[sc];
+      u.row[h] = ok ? (uint32_t)sc * a.page_size + (key - page_of(key, a.page_size, ps_inv) * a.page_size) : NO_ROW;
     }
     // keys without a row read the pools' first rows: their scores are masked
     if constexpr (EVEN) {
@@ -148,7 +142,8 @@ __global__ __launch_bounds__(64 * AW, DH == 64 ? 3 : 2) void cache_attn_kernel(c
   };
 
   // (the first unit's entries before the queries: neither waits for the other)
-  Entries ahead = entries(x0 + wave);
+  Entries ahead = {};
+  if (x0 + wave < x1) ahead = entries(x0 + wave);
   const int ul = min(u0 + n, pairs - 1), jl = ul / G, hq = hk * G + (ul - jl * G), pos = base + jl;  // this lane's pair
   f16x8_t q[KS][NP];
   const float qf = load_query<T, DH>(reinterpret_cast<const T*>(a.q) + (size_t)(r0 + jl) * a.ldq + (size_t)hq * DH, g,
@@ -159,14 +154,13 @@ __global__ __launch_bounds__(64 * AW, DH == 64 ? 3 : 2) void cache_attn_kernel(c
   f32x4_t o[NB];
 #pragma unroll
   for (int d = 0; d < NB; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  Unit<DH, EVEN> ua, ub;  // in turn: one in work, the other on its way
+  Unit<DH, EVEN> ua, ub, uc;  // in turn: one in work, the others on their way
 
-  // Unit x from `cur`; the wave's next one on its way to `next`.
+  // Unit x from `cur`; the wave's next but one on its way to `next`.
   auto step = [&](const Unit<DH, EVEN>& cur, Unit<DH, EVEN>& next, int x) {
-    if (x + AW < x1) {
-      request(next, x + AW, ahead);
-      ahead = entries(x + 2 * AW);
-    }
+    const Entries then = entries(x + 3 * AW);  // before the codes, for which it must not wait
+    request(next, x + 2 * AW, ahead);
+    ahead = then;
     const bool rows = EVEN ? cur.row[0] != NO_ROW && cur.row[NE - 1] != NO_ROW : __all(cur.row[0] != NO_ROW);
     const bool full = rows && x * UNIT + UNIT - 1 <= first;  // no key of it is masked
     float bias[8];
@@ -176,7 +170,13 @@ __global__ __launch_bounds__(64 * AW, DH == 64 ? 3 : 2) void cache_attn_kernel(c
         bias[i] = bias_row[max(0, min(pos - (x * UNIT + 16 * (i / 4) + 4 * g + i % 4), a.n_bias - 1))];
     }
     // scales over the unit's largest
-    float ktop = fmaxf(cur.ks[0], cur.ks[NE - 1]), vtop = fmaxf(cur.vs[0], cur.vs[NE - 1]);
+    float ks[NE], vs[NE];
+#pragma unroll
+    for (int h = 0; h < NE; ++h) {
+      ks[h] = cur.row[h] != NO_ROW ? cur.ks[h] : 0.f;
+      vs[h] = cur.row[h] != NO_ROW ? cur.vs[h] : 0.f;
+    }
+    float ktop = fmaxf(ks[0], ks[NE - 1]), vtop = fmaxf(vs[0], vs[NE - 1]);
     if constexpr (!EVEN) {
 #pragma unroll
       for (int i = 1; i < 32; i <<= 1) {
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(64 * AW, DH == 64 ? 3 : 2) void cache_attn_kernel(c
     f32x4_t s[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const float k = (EVEN ? cur.ks[h % NE] : __shfl(cur.ks[0], 16 * h + n, SSD_WAVE)) * kinv;
+      const float k = (EVEN ? ks[h % NE] : __shfl(ks[0], 16 * h + n, SSD_WAVE)) * kinv;
       const Ratio kr = ratio_of(k, k);
       s[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
       const uint32_t* kw = reinterpret_cast<const uint32_t*>(&cur.k[h][0]);
@@ -248,8 +248,8 @@ __global__ __launch_bounds__(64 * AW, DH == 64 ? 3 : 2) void cache_attn_kernel(c
 #pragma unroll
     for (int k = 0; k < 4; ++k) {  // keys 2 k and 2 k + 1 of the lane's eight
       const int src = 16 * (k / 2) + 4 * g + 2 * (k % 2);
-      if (EVEN) vr[k] = ratio_of(cur.vs[k / 2 % NE] * vinv, cur.vs[k / 2 % NE] * vinv);
-      else vr[k] = ratio_of(__shfl(cur.vs[0], src, SSD_WAVE) * vinv, __shfl(cur.vs[0], src + 1, SSD_WAVE) * vinv);
+      if (EVEN) vr[k] = ratio_of(vs[k / 2 % NE] * vinv, vs[k / 2 % NE] * vinv);
+      else vr[k] = ratio_of(__shfl(vs[0], src, SSD_WAVE) * vinv, __shfl(vs[0], src + 1, SSD_WAVE) * vinv);
     }
 #pragma unroll
     for (int i = 0; i < VW; ++i) {
@@ -263,11 +263,14 @@ __global__ __launch_bounds__(64 * AW, DH == 64 ? 3 : 2) void cache_attn_kernel(c
     }
   };
   if (x0 + wave < x1) {
+    Entries then = entries(x0 + wave + AW);
     request(ua, x0 + wave, ahead);
-    ahead = entries(x0 + wave + AW);
-    for (int x = x0 + wave; x < x1; x += 2 * AW) {
-      step(ua, ub, x);
+    ahead = entries(x0 + wave + 2 * AW);
+    request(ub, x0 + wave + AW, then);
+    for (int x = x0 + wave; x < x1; x += 3 * AW) {
+      step(ua, uc, x);
       if (x + AW < x1) step(ub, ua, x + AW);
+      if (x + 2 * AW < x1) step(uc, ub, x + 2 * AW);
     }
   }
   if (bad_page) atomicOr(a.status, SSD_DEV_BAD_PAGE);
@@ -407,16 +410,20 @@ hipError_t launch_t(const CacheAttnArgs& a, hipStream_t s) {
 
 }  // namespace
 
-// Key ranges a (row, head) pair's keys are split into: enough blocks to fill the 256 compute units,
-// while a range keeps 128 keys (one unit a wave).  Blocks of eight waves: one each.  Four waves: two
-// each (three of the few-row kernel with heads of 64, by their registers), but three for a batch in
-// the few-row kernel, whose ragged lengths leave some ranges empty (32 sequences of up to 4096
-// positions: 49 us against 54; one of 32768: 72 us against 60).
+// Key ranges a (row, head) pair's keys are split into: a block for each of the 256 compute units (two
+// of the 64-pair kernel's), while a range keeps 128 keys (one unit a wave).  Batches in the few-row
+// kernel take up to three blocks a unit, as long as a range keeps 1024 keys: ragged lengths leave
+// some ranges empty (32 sequences of up to 4096 positions: 42 us against 46; eight of up to 1000 and
+// nine rows each: 18 us against 15).
 int cache_attn_splits(const CacheAttnArgs& a) {
   const long long blocks = blocks_of(a);
   const int n = block_pairs(a);
-  const int per_cu = n >= 128 ? 1 : n == 16 && (a.d_head == 64 || a.B > 1) ? 3 : 2;
-  long long want = (256LL * per_cu + blocks - 1) / blocks;
+  long long want = (256LL * (n == 64 ? 2 : 1) + blocks - 1) / blocks;
+  if (n == 16 && a.B > 1) {
+    const long long even = (768 + blocks - 1) / blocks, most = a.max_len / 1024;
+    const long long more = even < most ? even : most;
+    if (want < more) want = more;
+  }
   const long long most = (a.max_len + AW * UNIT - 1) / (AW * UNIT);
   if (want > most) want = most;
   if (want > CACHE_SPLITS_MAX) want = CACHE_SPLITS_MAX;

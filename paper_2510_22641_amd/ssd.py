@@ -50,26 +50,39 @@ class ssd_kv(ctypes.Structure):
                 ("xv", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p)]
 
 
-class _Described(ctypes.Structure):
-    """A descriptor whose pointer fields also take tensors, as the calls' arguments do."""
+def _p(x):
+    if x is None or type(x) is int:
+        return x
+    if hasattr(x, "data_ptr"):
+        return x.data_ptr()
+    return int(x)
 
-    def __init__(self, *args, **kw):
-        kw.update(zip((n for n, _ in self._fields_), args))
-        pointers = {n for n, t in self._fields_ if t is c_void_p}
-        super().__init__(**{n: _p(v) if n in pointers else v for n, v in kw.items()})
 
-
-class ssd_cache(_Described):
+class ssd_cache(ctypes.Structure):
+    """An 8-bit cache of one layer; pointers may be tensors, as in the calls."""
     _fields_ = [(n, c_void_p) for n in ("k_codes", "v_codes", "k_scale", "v_scale")] + \
                [(n, c_int32) for n in ("n_pages", "n_heads", "page_size", "d_head")]
 
+    def __init__(self, k_codes=None, v_codes=None, k_scale=None, v_scale=None, n_pages=0, n_heads=0,
+                 page_size=0, d_head=0):
+        super().__init__(_p(k_codes), _p(v_codes), _p(k_scale), _p(v_scale), n_pages, n_heads,
+                         page_size, d_head)
 
-class ssd_cache_attn(_Described):
+
+class ssd_cache_attn(ctypes.Structure):
+    """An attention call's rows; pointers may be tensors, as in the calls."""
     _fields_ = [(n, c_int32) for n in ("B", "rows", "max_rows", "max_len", "n_q_heads", "dtype")] + \
                [("q", c_void_p), ("ldq", c_int64), ("out", c_void_p), ("ldo", c_int64),
                 ("row_start", c_void_p), ("seq_len", c_void_p), ("pos_off", c_int32),
                 ("max_pages", c_int32), ("page_table", c_void_p), ("bias", c_void_p),
                 ("n_bias", c_int32), ("scale", c_float), ("status", c_void_p)]
+
+    def __init__(self, B=0, rows=0, max_rows=0, max_len=0, n_q_heads=0, dtype=0, q=None, ldq=0,
+                 out=None, ldo=0, row_start=None, seq_len=None, pos_off=0, max_pages=0,
+                 page_table=None, bias=None, n_bias=0, scale=0.0, status=None):
+        super().__init__(B, rows, max_rows, max_len, n_q_heads, dtype, _p(q), ldq, _p(out), ldo,
+                         _p(row_start), _p(seq_len), pos_off, max_pages, _p(page_table), _p(bias),
+                         n_bias, scale, _p(status))
 
 
 class SSDError(RuntimeError):
@@ -138,14 +151,6 @@ EXPORTS = ("ssd_workspace_bytes", "ssd_create", "ssd_create_static", "ssd_prefil
            "ssd_cache_load", "ssd_cache_attention_workspace", "ssd_cache_attention",
            "ssd_sync_status",
            "ssd_status_string", "ssd_destroy")
-
-
-def _p(x):
-    if x is None:
-        return None
-    if hasattr(x, "data_ptr"):
-        return x.data_ptr()
-    return int(x)
 
 
 def _check(fn, rc):
