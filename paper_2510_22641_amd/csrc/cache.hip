@@ -14,7 +14,6 @@ namespace ssd {
 namespace {
 
 constexpr int MAP_THREADS = 256;
-constexpr int MAP_ROWS = 1024;  // rows a block writes slots for
 
 // Exclusive prefix sums over the block's threads of one value each; *total receives the sum.
 __device__ __forceinline__ long long block_scan(long long v, long long* waves, long long* total) {
@@ -52,89 +51,92 @@ __device__ __forceinline__ int find_seq(const int* start, int B, int r) {
 // sums over the sequences (a few loads a thread), so that one launch does it all: no block waits for
 // another, and a new page's id comes from the free list by its rank instead of from the table that
 // other blocks are writing.  Then a block writes its share of the new table entries and the slots
-// of its MAP_ROWS rows, each finding its sequence by bisection in LDS.  Bound: launch latency and
+// of its 256 rows, each finding its sequence by bisection in LDS.  Bound: launch latency and
 // one dependent chain (lengths, sums, table entry), not bytes.
-__global__ __launch_bounds__(MAP_THREADS) void page_map_kernel(const PageMapArgs a) {
+__global__ __launch_bounds__(MAP_THREADS) void page_map_kernel(const PageMapArgs a, const uint32_t ps_inv) {
   extern __shared__ int map_lds[];
   int* row0 = map_lds;               // [B + 1] first row of each sequence
   int* page0 = map_lds + a.B + 1;    // [B + 1] rank in the free list of its first new page
+  int* len0 = page0 + a.B + 1;       // [B] positions it holds
   __shared__ long long waves[MAP_THREADS / 64];
   const int tid = threadIdx.x;
   const int cap = a.cap;
   int fault = 0;
-  // pages of a sequence with `len` positions held and n new rows: [first, end) of its table row
+  auto pages_of = [&](int positions) { return page_of(positions + a.page_size - 1, a.page_size, ps_inv); };  // <= cap
+  // pages of a sequence with `len` positions held and n new rows: the first and how many
   auto need = [&](int len, int n, int& first) {
     first = 0;
     if (!a.free_pages || len < 0 || len > cap || n <= 0) return 0;
-    first = (len + a.page_size - 1) / a.page_size;
-    const long long end = (long long)len + n < cap ? (long long)len + n : cap;
-    return (int)((end + a.page_size - 1) / a.page_size) - first;
+    first = pages_of(len);
+    return pages_of(n < cap - len ? len + n : cap) - first;
   };
-  long long rows = 0, pages = 0;
-  for (int b0 = 0; b0 < a.B; b0 += MAP_THREADS) {
-    const int b = b0 + tid;
-    int len = 0, n = 0;
-    if (b < a.B) {
-      len = a.seq_len[b] + a.pos_off;
-      n = a.new_rows ? a.new_rows[b] : a.new_const;
-      if (n < 0) { n = 0; fault = 1; }
-      if (len < 0 || (long long)len + n > cap) fault |= n > 0;
-    }
-    long long sum;
-    const long long r0 = rows + block_scan(n, waves, &sum);
-    rows += sum;
+  // counts and lengths first, where the sums will be
+  for (int b = tid; b < a.B; b += MAP_THREADS) {
+    const int len = a.seq_len[b] + a.pos_off, n = a.new_rows ? a.new_rows[b] : a.new_const;
+    if (n < 0 || (n > 0 && (len < 0 || (long long)len + n > cap))) fault = 1;
+    row0[b] = max(n, 0);
+    len0[b] = len;
+  }
+  __syncthreads();
+  // a thread takes `per` sequences one after the other
+  const int per = (a.B + MAP_THREADS - 1) / MAP_THREADS, b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
+  long long rows, pages, sum = 0;
+  for (int b = b0; b < b1; ++b) sum += row0[b];
+  long long r = block_scan(sum, waves, &rows);
+  sum = 0;
+  for (int b = b0; b < b1; ++b) {
     // rows past max_rows are cut: they get no slot and no page
-    const int r_lo = (int)(r0 < a.max_rows ? r0 : a.max_rows);
-    const int r_hi = (int)(r0 + n < a.max_rows ? r0 + n : a.max_rows);
+    const int lo = (int)(r < a.max_rows ? r : a.max_rows);
+    r += row0[b];
     int first;
-    const long long p0 = pages + block_scan(need(len, r_hi - r_lo, first), waves, &sum);
-    pages += sum;
-    if (b < a.B) {
-      row0[b] = r_lo;
-      page0[b] = (int)(p0 < a.n_free ? p0 : a.n_free);
-    }
+    sum += need(len0[b], (int)(r < a.max_rows ? r : a.max_rows) - lo, first);
+    row0[b] = lo;
+  }
+  if (tid == 0) row0[a.B] = (int)(rows < a.max_rows ? rows : a.max_rows);
+  long long p = block_scan(sum, waves, &pages);  // (and its barriers: every row0 is in place)
+  for (int b = b0; b < b1; ++b) {
+    int first;
+    const int n = need(len0[b], row0[b + 1] - row0[b], first);
+    page0[b] = (int)(p < a.n_free ? p : a.n_free);
+    p += n;
   }
   if (rows > a.max_rows || pages > a.n_free) fault = 1;
   const int n_rows = (int)(rows < a.max_rows ? rows : a.max_rows);
   const int n_pages = (int)(pages < a.n_free ? pages : a.n_free);
-  if (tid == 0) {
-    row0[a.B] = n_rows;
-    page0[a.B] = n_pages;
-  }
+  if (tid == 0) page0[a.B] = n_pages;
   __syncthreads();
   if (blockIdx.x == 0) {
+    if (fault) atomicOr(a.status, SSD_DEV_CAPACITY);  // (each thread knows of its own)
     if (a.row_start)
       for (int b = tid; b <= a.B; b += MAP_THREADS) a.row_start[b] = row0[b];
     if (tid == 0 && a.taken) *a.taken = n_pages;
-    if (fault) atomicOr(a.status, SSD_DEV_CAPACITY);
   }
   // new table entries: rank t of the free list belongs to the sequence with page0[b] <= t
   for (int t = blockIdx.x * MAP_THREADS + tid; t < n_pages; t += gridDim.x * MAP_THREADS) {
     const int b = find_seq(page0, a.B, t);
     int first;
-    need(a.seq_len[b] + a.pos_off, row0[b + 1] - row0[b], first);
+    need(len0[b], row0[b + 1] - row0[b], first);
     a.page_table[(size_t)b * a.max_pages + first + t - page0[b]] = a.free_pages[t];
   }
   // entries that the free list could not fill: the last sequences' (none unless `fault`)
   if (a.free_pages && pages > a.n_free && blockIdx.x == 0) {
     for (int b = tid; b < a.B; b += MAP_THREADS) {
       int first;
-      const int n = need(a.seq_len[b] + a.pos_off, row0[b + 1] - row0[b], first);
+      const int n = need(len0[b], row0[b + 1] - row0[b], first);
       for (int i = page0[b + 1] - page0[b]; i < n; ++i) a.page_table[(size_t)b * a.max_pages + first + i] = -1;
     }
   }
   if (!a.slot) return;
-#pragma unroll
-  for (int u = 0; u < MAP_ROWS / MAP_THREADS; ++u) {
-    const int r = blockIdx.x * MAP_ROWS + u * MAP_THREADS + tid;
-    if (r >= a.max_rows) break;
+  {
+    const int r = blockIdx.x * MAP_THREADS + tid;
+    if (r >= a.max_rows) return;
     int64_t s = -1;
     if (r < n_rows) {
       const int b = find_seq(row0, a.B, r);
-      const int len = a.seq_len[b] + a.pos_off;
+      const int len = len0[b];
       const long long p = (long long)len + r - row0[b];
       if (len >= 0 && p < cap) {
-        const int i = (int)(p / a.page_size);
+        const int i = page_of((int)p, a.page_size, ps_inv);
         int first;
         const int n = need(len, row0[b + 1] - row0[b], first);
         int page;
@@ -149,7 +151,7 @@ __global__ __launch_bounds__(MAP_THREADS) void page_map_kernel(const PageMapArgs
           atomicOr(a.status, SSD_DEV_BAD_PAGE);
           page = -1;
         }
-        if (page >= 0) s = (int64_t)page * a.page_size + p % a.page_size;
+        if (page >= 0) s = (int64_t)page * a.page_size + ((int)p - i * a.page_size);
       }
     }
     a.slot[r] = s;
@@ -455,8 +457,9 @@ hipError_t store_t(const CacheRowsArgs& a, int window, int groups, dim3 grid, hi
 
 hipError_t launch_page_map(const PageMapArgs& a, hipStream_t s) {
   if (a.B < 1 || a.B > PAGE_MAP_MAX_BATCH) return hipErrorInvalidValue;
-  const int blocks = a.max_rows > MAP_ROWS ? (a.max_rows + MAP_ROWS - 1) / MAP_ROWS : 1;
-  hipLaunchKernelGGL(page_map_kernel, dim3(blocks), dim3(MAP_THREADS), 2 * (a.B + 1) * sizeof(int), s, a);
+  const int blocks = a.max_rows > MAP_THREADS ? (a.max_rows + MAP_THREADS - 1) / MAP_THREADS : 1;
+  hipLaunchKernelGGL(page_map_kernel, dim3(blocks), dim3(MAP_THREADS), (3 * a.B + 2) * sizeof(int), s, a,
+                     page_inv(a.page_size));
   return hipGetLastError();
 }
 

@@ -198,12 +198,6 @@ __device__ __forceinline__ void store_out(T* o, const float* f, bool vec) {
 // (Row (page n_heads + head) page_size + offset of the pools; there are fewer than 2^32 of them.)
 constexpr uint32_t NO_ROW = 0xffffffffu;
 
-// i / page_size for i < 2^24, page_size <= 256, with inv = ceil(2^32 / page_size) (page_size 1: the
-// quotient is i)
-__device__ __forceinline__ int page_of(int i, int page_size, uint32_t inv) {
-  return page_size == 1 ? i : (int)__umulhi((uint32_t)i, inv);
-}
-
 // The running reference of a row's softmax.  Scores are t = s * f (+ bias); without a bias f carries
 // log2 e and t is in powers of two, with one t stays in natural units, where the type's lowest value
 // is a finite number (times log2 e it would not be).

@@ -394,7 +394,7 @@ hipError_t launch_t(const CacheAttnArgs& a, hipStream_t s) {
   } else {
     const dim3 grid((unsigned)blocks_of(a), splits), block(64 * AW);
     const int tiles = (int)((pairs_of(a) + 15) / 16);
-    const uint32_t inv = (uint32_t)(((1ull << 32) + a.page_size - 1) / a.page_size);
+    const uint32_t inv = page_inv(a.page_size);
 #define LAUNCH(BIAS, EVEN) \
   hipLaunchKernelGGL((cache_attn_kernel<T, DH, BIAS, EVEN>), grid, block, 0, s, a, tiles, splits, inv)
     const bool even = a.page_size % 16 == 0;

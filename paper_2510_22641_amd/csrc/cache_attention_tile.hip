@@ -349,7 +349,7 @@ template <typename T, int DH, int NT, int TW>
 void launch_tw(const CacheAttnArgs& a, int splits, hipStream_t s) {
   const int pairs = a.max_rows * (a.n_q_heads / a.n_heads), tiles = (pairs + 16 * NT * TW - 1) / (16 * NT * TW);
   const dim3 grid((unsigned)((size_t)a.B * tiles * a.n_heads), splits), block(64 * TW);
-  const uint32_t inv = (uint32_t)(((1ull << 32) + a.page_size - 1) / a.page_size);
+  const uint32_t inv = page_inv(a.page_size);
   if (a.bias) hipLaunchKernelGGL((cache_attn_tile_kernel<T, DH, true, NT, TW>), grid, block, 0, s, a, tiles, splits, inv);
   else hipLaunchKernelGGL((cache_attn_tile_kernel<T, DH, false, NT, TW>), grid, block, 0, s, a, tiles, splits, inv);
 }

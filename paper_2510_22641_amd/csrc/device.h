@@ -136,6 +136,12 @@ __device__ __forceinline__ void wave_argmax(float& v, int& i) {
   }
 }
 
+// i / page_size for i < 2^24, page_size <= 256, with inv = ceil(2^32 / page_size) (page_size 1: the
+// quotient is i)
+__device__ __forceinline__ int page_of(int i, int page_size, uint32_t inv) {
+  return page_size == 1 ? i : (int)__umulhi((uint32_t)i, inv);
+}
+
 // tanh form of GELU (T5-v1.1 gated FFN, imitation network)
 __device__ __forceinline__ float gelu_tanh(float u) {
   const float c = 0.7978845608028654f;  // sqrt(2/pi)

@@ -370,6 +370,8 @@ hipError_t launch_bias_table(const float* rel_bias, const int32_t* bucket, int H
 constexpr int PAGE_MAP_MAX_BATCH = 4096;  // two prefix sums over the sequences in LDS
 constexpr int CACHE_MAX_PAGE = 256;       // positions per page
 constexpr int CACHE_SPLITS_MAX = 64;
+// The factor of page_of (device.h).
+inline uint32_t page_inv(int page_size) { return (uint32_t)(((1ull << 32) + page_size - 1) / page_size); }
 
 struct PageMapArgs {
   int B, page_size, n_pages, max_pages;
