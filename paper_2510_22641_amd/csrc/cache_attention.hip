@@ -10,7 +10,6 @@ namespace ssd {
 
 namespace {
 
-constexpr int AW = 4;     // waves a block
 constexpr int UNIT = 32;  // keys a wave takes at once
 
 // What a wave needs of a unit before its products: codes as loaded, and scales.
@@ -42,8 +41,8 @@ __device__ __forceinline__ V scalar_load(const V* p) {
 // scalars; else every key has its own, which cross lanes.  Each wave keeps its own reference, sum
 // and largest value scale; they meet in LDS once.
 // Bound: bytes of codes for long contexts, the chain lengths -> table -> codes for short ones.
-template <typename T, int DH, bool BIAS, bool EVEN>
-__global__ __launch_bounds__(64 * AW, DH == 64 ? 3 : 2) void cache_attn_kernel(const CacheAttnArgs a, const int tiles,
+template <typename T, int DH, bool BIAS, bool EVEN, int AW>
+__global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_attn_kernel(const CacheAttnArgs a, const int tiles,
                                                                                const int splits, const uint32_t ps_inv) {
   constexpr int KS = DH / 32;  // steps of 32 over d_head
   constexpr int NB = DH / 16;  // output blocks of 16 dimensions
@@ -289,7 +288,7 @@ __global__ __launch_bounds__(64 * AW, DH == 64 ? 3 : 2) void cache_attn_kernel(c
   constexpr int PART = DH / 16;
   const int pn = tid >> 4, d0 = (tid & 15) * PART;
   const int pu = u0 + pn;
-  if (pu >= pairs) return;
+  if (pn >= 16 || pu >= pairs) return;
   float M = xm[0][pn];
 #pragma unroll
   for (int w = 1; w < AW; ++w) M = fmaxf(M, xm[w][pn]);
@@ -392,11 +391,19 @@ hipError_t launch_t(const CacheAttnArgs& a, hipStream_t s) {
   if (n >= 64) {
     e = launch_cache_attn_tile(a, n, splits, s);
   } else {
-    const dim3 grid((unsigned)blocks_of(a), splits), block(64 * AW);
+    const dim3 grid((unsigned)blocks_of(a), splits);
     const int tiles = (int)((pairs_of(a) + 15) / 16);
     const uint32_t inv = page_inv(a.page_size);
-#define LAUNCH(BIAS, EVEN) \
-  hipLaunchKernelGGL((cache_attn_kernel<T, DH, BIAS, EVEN>), grid, block, 0, s, a, tiles, splits, inv)
+    // eight waves where that leaves each two units of the longest range (eight requests of up to 1000
+    // positions and nine rows each: 13.5 us against 15.4), four for shorter ones (70 positions: 5.7
+    // against 5.8)
+    const int waves = a.max_len / splits >= 16 * UNIT ? 8 : 4;
+    const dim3 block(64 * waves);
+#define LAUNCH(BIAS, EVEN)                                                                                          \
+  do {                                                                                                              \
+    if (waves == 8) hipLaunchKernelGGL((cache_attn_kernel<T, DH, BIAS, EVEN, 8>), grid, block, 0, s, a, tiles, splits, inv); \
+    else hipLaunchKernelGGL((cache_attn_kernel<T, DH, BIAS, EVEN, 4>), grid, block, 0, s, a, tiles, splits, inv);            \
+  } while (0)
     const bool even = a.page_size % 16 == 0;
     if (a.bias) { if (even) LAUNCH(true, true); else LAUNCH(true, false); }
     else { if (even) LAUNCH(false, true); else LAUNCH(false, false); }
@@ -411,20 +418,13 @@ hipError_t launch_t(const CacheAttnArgs& a, hipStream_t s) {
 }  // namespace
 
 // Key ranges a (row, head) pair's keys are split into: a block for each of the 256 compute units (two
-// of the 64-pair kernel's), while a range keeps 128 keys (one unit a wave).  Batches in the few-row
-// kernel take up to three blocks a unit, as long as a range keeps 1024 keys: ragged lengths leave
-// some ranges empty (32 sequences of up to 4096 positions: 42 us against 46; eight of up to 1000 and
-// nine rows each: 18 us against 15).
+// of the 64-pair kernel's four waves), while a range keeps 128 keys.  More of them measured no
+// faster (one token of 32 heads over 32768 positions: 58 us with 256 blocks of eight waves, 64 with
+// 512; 32 tokens of 8 cache heads: 43 against 50).
 int cache_attn_splits(const CacheAttnArgs& a) {
   const long long blocks = blocks_of(a);
-  const int n = block_pairs(a);
-  long long want = (256LL * (n == 64 ? 2 : 1) + blocks - 1) / blocks;
-  if (n == 16 && a.B > 1) {
-    const long long even = (768 + blocks - 1) / blocks, most = a.max_len / 1024;
-    const long long more = even < most ? even : most;
-    if (want < more) want = more;
-  }
-  const long long most = (a.max_len + AW * UNIT - 1) / (AW * UNIT);
+  long long want = (256LL * (block_pairs(a) == 64 ? 2 : 1) + blocks - 1) / blocks;
+  const long long most = (a.max_len + 127) / 128;
   if (want > most) want = most;
   if (want > CACHE_SPLITS_MAX) want = CACHE_SPLITS_MAX;
   return want < 1 ? 1 : (int)want;
