@@ -420,13 +420,16 @@ hipError_t launch_t(const CacheAttnArgs& a, hipStream_t s) {
 // Key ranges a (row, head) pair's keys are split into: a block for each of the 256 compute units (two
 // of the 64-pair kernel's four waves), while a range keeps 128 keys.  More of them measured no
 // faster (one token of 32 heads over 32768 positions: 58 us with 256 blocks of eight waves, 64 with
-// 512; 32 tokens of 8 cache heads: 43 against 50).
+// 512; 32 tokens of 8 cache heads: 43 against 50).  The few-row kernel keeps short ranges whole, where
+// the merge would cost more than the waves save (one token of 32 heads of 128: 300 positions 8.7 us
+// whole, 9.6 in three ranges; 1000: 13.6 and 9.7 in eight; four tokens, 1000: 15.1 and 16.1 in two).
 int cache_attn_splits(const CacheAttnArgs& a) {
   const long long blocks = blocks_of(a);
   long long want = (256LL * (block_pairs(a) == 64 ? 2 : 1) + blocks - 1) / blocks;
   const long long most = (a.max_len + 127) / 128;
   if (want > most) want = most;
   if (want > CACHE_SPLITS_MAX) want = CACHE_SPLITS_MAX;
+  if (block_pairs(a) == 16 && (a.max_len <= 512 || (want < 4 && a.max_len < 2048))) want = 1;
   return want < 1 ? 1 : (int)want;
 }
 
