@@ -42,7 +42,7 @@ def cached(c, layer, b, n):
     return out
 
 
-def attend_reference(c, layer, q, starts, counts, scale, bias=None):
+def attend_reference(c, layer, q, starts, counts, scale, bias=None, apart=False):
     """(output, bound of the error) in float64 from the cache's own values.
 
     Bound.  A score is a sum of d_head products in float32 (the planes of a float32 query hold its
@@ -53,7 +53,15 @@ def attend_reference(c, layer, q, starts, counts, scale, bias=None):
     add n 2^-24 each.  Float32 queries and weights enter the products as two f16 planes, each within
     2^-11 of what it rounds: 2^-22 in all, of sum |q k| scale and of the weights.  bf16 queries are
     exact in one plane (8 bits in 11); their weights are one plane, within 2^-11, and the output is
-    rounded once (2^-8)."""
+    rounded once (2^-8).
+
+    apart: blocks of scales more than 2^24 apart among 64 keys.  A code times its scale's ratio to
+    the largest is held in f16, whose step below 2^-14 is 2^-24: it is off by at most 2^-25 of the
+    largest scale, which moves a score by at most sum |q| scale 2^-25 times that of the keys, and
+    an output by 2^-25 times that of the values.  A weight, 2^7 times its value, meets the same step:
+    it is off by at most 2^-32 of the row's largest whatever its own size, so a key by 2^-32 times
+    its value, at most 127 times the largest scale: 2^-25 of it for each of the keys, where the
+    values that carry the weight may be far smaller."""
     H, G = c.n_heads, q.shape[1] // c.n_heads
     q64 = q.double().cpu()
     out, tol = torch.zeros_like(q64), torch.zeros_like(q64)
@@ -76,6 +84,10 @@ def attend_reference(c, layer, q, starts, counts, scale, bias=None):
             top = torch.where(some, x.amax(1) if N else torch.zeros(n), 0.0)
             w = torch.exp(x - top[:, None])
             ds = torch.where(x > -math.inf, (c.d_head + 6 + 4) * u * mag, 0.0).amax(1) if N else torch.zeros(n)
+            if apart:
+                pages = c.page_table[b, :-(-N // c.page_size)].long()
+                kt, vt = (float(t[layer, pages, h // G].max()) for t in (c.k_scale, c.v_scale))
+                ds = ds + qh.abs().sum(1) * abs(scale) * 2.0 ** -25 * kt
             gap = torch.where(w > 1e-8, top[:, None] - x, 0.0).amax(1) if N else torch.zeros(n)
             L = w.sum(1)
             inv = torch.where(some, 1 / L, 0.0)[:, None]
@@ -83,20 +95,20 @@ def attend_reference(c, layer, q, starts, counts, scale, bias=None):
             e = 2 * ds + (gap + 6) * u
             near = (w @ vh.abs()) * inv
             extra = 2.0 ** (-22 if q.dtype == F32 else -11)
-            tol[r:r + n, h] = near * (2 * e + 2 * (N + 8) * u + extra)[:, None] + 1e-30
+            tol[r:r + n, h] = near * (2 * e + 2 * (N + 8) * u + extra)[:, None] + ((N + 1) * 2.0 ** -25 * vt if apart else 0.0) + 1e-30
         r += n
     if q.dtype == BF16:
         tol = tol + (out.abs() + tol) * 2.0 ** -8
     return out, tol
 
 
-def check_attend(c, q, new, scale, bias=None, layer=0, row_start=None, out=None, fill=None):
+def check_attend(c, q, new, scale, bias=None, layer=0, row_start=None, out=None, apart=False):
     """The call on the last new[b] rows of each sequence against the reference."""
     if row_start is None:
         row_start = torch.tensor([0] + list(np.cumsum(new)), dtype=torch.int32, device="cuda")
     starts = [l - n for l, n in zip(c.lens, new)]
     got = c.attend(layer, q, row_start, max(max(new), 1), scale, bias, out)
-    ref, tol = attend_reference(c, layer, q, starts, new, scale, bias)
+    ref, tol = attend_reference(c, layer, q, starts, new, scale, bias, apart)
     err = (got.double().cpu() - ref).abs()
     assert bool((err <= tol).all()), (float((err - tol).max()), float((err / tol).max()))
     assert int(c.status) == 0
@@ -489,6 +501,60 @@ def test_many_sequences_and_one_long_one():
     c.grow([5])
     for dt in (F32, BF16):
         check_attend(c, torch.randn(5, 4, 128, generator=g).to(dt).cuda(), [5], 0.09)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("lens,new,heads,group,d_head,page", [
+    # eight waves a block, whole and split; even and odd pages
+    ([600 + i for i in range(70)], [1] * 70, 4, 1, 64, 16), ([650 - i for i in range(33)], [2] * 33, 8, 3, 128, 7),
+    ([40000], [1], 1, 4, 128, 16), ([40000], [3], 1, 1, 64, 5),
+    # four waves, in ranges
+    ([900], [1], 2, 1, 128, 16), ([1023], [7], 2, 2, 64, 9),
+    # blocks of 64 pairs with ranges, of 128, of 256 with and without rows left over
+    ([2000, 5], [17, 21], 2, 3, 128, 16), ([70, 0], [65, 128], 4, 1, 128, 16), ([30], [129], 1, 1, 64, 3),
+    ([10, 77], [300, 257], 64, 1, 64, 16), ([33], [260], 128, 1, 128, 5)])
+def test_attention_of_every_launch_shape(lens, new, heads, group, d_head, page, dtype):
+    c, g = make_cache(lens, heads, d_head, page, max_seq=max(l + n for l, n in zip(lens, new)) + 1)
+    c.grow(new)
+    q = torch.randn(sum(new), heads * group, d_head, generator=g).to(dtype).cuda()
+    check_attend(c, q, new, -(d_head ** -0.5))  # (a negative factor is a factor)
+    bias = torch.randn(heads * group, 300, generator=g).cuda()
+    check_attend(c, (q.float() / 8).to(dtype), new, 1.0, bias)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,page", [(1, 16), (1, 3), (9, 16), (40, 16), (140, 5)])
+def test_attention_over_blocks_of_scales_far_apart(rows, page, dtype):
+    c, g = make_cache([210, 15], 2, 128, page, max_seq=400)
+    for t in (c.k_scale, c.v_scale):
+        t.copy_(torch.exp2(torch.randint(-45, -3, t.shape, generator=g).float()))
+    c.grow([rows, rows])
+    q = torch.randn(2 * rows, 4, 128, generator=g).to(dtype).cuda()
+    check_attend(c, q, [rows, rows], 0.5, apart=True)
+    # one range of magnitudes for all, however small or large
+    for e in (-99, 90):
+        c.k_scale.fill_(2.0 ** -e)
+        c.v_scale.fill_(2.0 ** e)
+        check_attend(c, (q.float() * 2.0 ** (e - 9)).to(dtype), [rows, rows], 1.0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows", [1, 30, 200])
+def test_attention_of_queries_of_zeros_infinities_and_no_factor(rows, dtype):
+    c, g = make_cache([50], 2, 64, 16, max_seq=400)
+    c.grow([rows])
+    q = torch.randn(rows, 2, 64, generator=g).to(dtype).cuda()
+    q[0, 0] = 0                                     # equal scores: the mean of the values
+    check_attend(c, q, [rows], 0.125)
+    check_attend(c, q, [rows], 0.0)
+    rs = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    out = c.attend(0, q, rs, rows, 0.125)
+    bad = q.clone()
+    bad[rows - 1, 1, 3] = math.inf
+    got = c.attend(0, bad, rs, rows, 0.125)
+    assert bool(got[rows - 1, 1].isnan().all())
+    got[rows - 1, 1] = out[rows - 1, 1]
+    assert torch.equal(got, out)
 
 
 def test_pools_past_32_bits():
