@@ -4,7 +4,6 @@
 // 0 .. p of its pages; the scores are q . c s_k scale + bias[h][p - i] with c the key's codes and s_k
 // its block's scale, the output sum_i w_i s_v c_i over the softmax weights w.
 #include "cache_attention.h"
-#include <type_traits>
 
 namespace ssd {
 
@@ -436,6 +435,16 @@ int cache_attn_splits(const CacheAttnArgs& a) {
 size_t cache_attn_part_floats(const CacheAttnArgs& a) {
   const int splits = cache_attn_splits(a);
   return splits > 1 ? (size_t)a.rows * a.n_q_heads * splits * (a.d_head + 2) : 0;
+}
+
+// Blocks of n pairs hold rows * n_q_heads <= blocks n pairs, and a split call has blocks * splits <
+// 256 + blocks <= 512 of them (n <= 128), or with n = 64 < 512 + blocks <= 1024: 2^16 splits of a pair.
+size_t cache_attn_part_bound(size_t rows, int n_q_heads, int d_head, int max_len) {
+  size_t splits = ((size_t)max_len + 127) / 128;
+  if (splits > CACHE_SPLITS_MAX) splits = CACHE_SPLITS_MAX;
+  if (splits < 2) return 0;
+  const size_t n = rows * n_q_heads * splits;
+  return (n < 1 << 16 ? n : 1 << 16) * (d_head + 2);
 }
 
 hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t s) {

@@ -436,6 +436,8 @@ struct CacheAttnArgs {
 };
 int cache_attn_splits(const CacheAttnArgs& a);
 size_t cache_attn_part_floats(const CacheAttnArgs& a);
+// At least those of every call of up to `rows` rows with max_len.
+size_t cache_attn_part_bound(size_t rows, int n_q_heads, int d_head, int max_len);
 hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t s);
 // Many rows: blocks of n (row, head) pairs (64, 128 or 256), without the merge of the splits.
 hipError_t launch_cache_attn_tile(const CacheAttnArgs& a, int n, int splits, hipStream_t s);

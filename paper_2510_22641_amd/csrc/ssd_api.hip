@@ -84,19 +84,6 @@ CacheAttnArgs cache_attn_of(const ssd_dims& d, int B, int C) {
   return a;
 }
 
-// Most floats of partial results that a pass of this context's attention may need.
-size_t cache_part_max(const ssd_dims& d) {
-  const int C1 = d.max_gamma + 1 > ctx_len_max(d) ? d.max_gamma + 1 : ctx_len_max(d);
-  size_t most = 0;
-  for (int B = 1; B <= d.max_batch; ++B)
-    for (int C = 1; C <= C1; ++C) {
-      const size_t n = cache_attn_part_floats(cache_attn_of(d, B, C));
-      if (n == 0) break;  // more rows are split no further
-      if (n > most) most = n;
-    }
-  return most;
-}
-
 // Workspace layout: the scratch a chain of launches writes (residual rows, projections, operand
 // planes, argmax partials, the layer-k stash ...), the tables, the folded cross-attention and
 // the loop state of ssd_generate, each slice 256-byte aligned.  Without allow_fold the
@@ -148,7 +135,7 @@ bool make_layout(const ssd_dims& d, Layout& L, bool allow_fold = true, bool allo
     // 8-bit caches: a pass's keys and values in float32, their slots, the attention's partials
     L.kv_rows = take(i8 ? 2 * R * HD * 4 : 0);
     L.kv_slot = take(i8 ? R * 8 : 0);
-    L.cache_part = take(i8 ? cache_part_max(d) * 4 : 0);
+    L.cache_part = take(i8 ? cache_attn_part_bound(rows, d.n_heads, d.d_head, d.max_seq) * 4 : 0);
   }
   L.vis = take(d.arch == SSD_ARCH_T5 ? B * (size_t)d.n_visual * D * 4 : 0);
   {
@@ -188,6 +175,11 @@ bool make_layout(const ssd_dims& d, Layout& L, bool allow_fold = true, bool allo
 bool cache_pages_ok(int page_size, int max_pages) {
   return page_size >= 1 && page_size <= CACHE_MAX_PAGE && max_pages >= 1 &&
          (long long)max_pages * page_size <= 1 << 24;
+}
+
+// Rows of the pools, which those kernels count in 32 bits.
+bool cache_rows_ok(int n_pages, int n_heads, int page_size) {
+  return (uint64_t)n_pages * n_heads * page_size < UINT32_MAX;
 }
 
 bool dims_ok(const ssd_dims* d) {
@@ -878,6 +870,7 @@ int check_create_args(const ssd_dims* dims, const ssd_weights* w, const ssd_kv* 
   if (d.kvdtype == SSD_I8 &&
       (!kv->k_scale || !kv->v_scale || (uintptr_t)kv->k_pool % 16 || (uintptr_t)kv->v_pool % 16))
     return SSD_ERR_ARG;
+  if (d.kvdtype == SSD_I8 && !cache_rows_ok(kv->n_pages, d.n_heads, d.page_size)) return SSD_ERR_SHAPE;
   return SSD_OK;
 }
 
@@ -968,7 +961,7 @@ struct StreamDevice {
 bool cache_shape_ok(const ssd_cache* c) {
   return c->n_pages >= 1 && c->n_heads >= 1 && c->n_heads <= 4096 && c->page_size >= 1 &&
          c->page_size <= CACHE_MAX_PAGE && (c->d_head == 64 || c->d_head == 128) &&
-         (uint64_t)c->n_pages * c->n_heads * c->page_size < UINT32_MAX;
+         cache_rows_ok(c->n_pages, c->n_heads, c->page_size);
 }
 
 bool cache_pointers_ok(const ssd_cache* c) {

@@ -34,7 +34,8 @@ class PagedCache:
     page and head (``ssd_cache``), a page table, and the pages not yet in use.
 
     ``grow`` gives sequences new positions, ``append`` stores their rows, ``attend`` attends them
-    and ``rows`` reads them back.  All run on torch's current stream of the device.
+    and ``rows`` reads them back.  All run on torch's current stream of the device, whichever device
+    is current; their tensors must have been made or waited for on that stream.
     """
 
     def __init__(self, n_layers: int, n_heads: int, d_head: int, max_batch: int, max_seq: int,
@@ -62,8 +63,12 @@ class PagedCache:
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self._workspace = torch.empty(0, dtype=torch.uint8, device=self.device)
 
-    def _stream(self) -> int:
-        return torch.cuda.current_stream(self.device).cuda_stream
+    def _call(self, fn, *args):
+        """A library call on torch's current stream of the device (its null stream is the current
+        device's)."""
+        stream = torch.cuda.current_stream(self.device).cuda_stream
+        with torch.cuda.device(self.device):
+            return fn(*args, stream)
 
     def _rows(self, t: torch.Tensor, heads: int, name: str) -> int:
         """Row stride of t [rows, heads, d_head], whose rows are contiguous."""
@@ -100,9 +105,9 @@ class PagedCache:
         counts = torch.tensor(list(new), dtype=torch.int32, device=self.device)
         row_start = torch.empty(B + 1, dtype=torch.int32, device=self.device)
         slot = torch.empty(sum(new), dtype=torch.int64, device=self.device)
-        abi.ssd_page_map(B, ps, self.n_pages, self.max_pages, self.seq_len, counts,
-                         self.free[self.used:] if need else None, need, self.page_table, row_start,
-                         slot, sum(new), self.taken, self.status, self._stream())
+        self._call(abi.ssd_page_map, B, ps, self.n_pages, self.max_pages, self.seq_len, counts,
+                   self.free[self.used:] if need else None, need, self.page_table, row_start, slot,
+                   sum(new), self.taken, self.status)
         self.used += need
         for b, n in enumerate(new):
             self.lens[b] += n
@@ -115,8 +120,8 @@ class PagedCache:
         if self._rows(v, self.n_heads, "v") != ld or v.shape != k.shape or v.dtype != k.dtype:
             raise ValueError("k and v of one layout expected")
         self._slots(slot, k.shape[0])
-        abi.ssd_cache_store(self._layer(layer), k.shape[0], slot, k, v, ld, self._dtype(k),
-                            self.status, self._stream())
+        self._call(abi.ssd_cache_store, self._layer(layer), k.shape[0], slot, k, v, ld,
+                   self._dtype(k), self.status)
 
     def rows(self, layer: int, slot: torch.Tensor, dtype: torch.dtype = torch.float32):
         """The values of cached rows: (k, v) [rows, heads, d_head]."""
@@ -124,8 +129,8 @@ class PagedCache:
         v = torch.zeros_like(k)
         ld = self._rows(k, self.n_heads, "dtype")
         self._slots(slot, slot.numel())
-        abi.ssd_cache_load(self._layer(layer), slot.numel(), slot, k, v, ld, self._dtype(k),
-                           self.status, self._stream())
+        self._call(abi.ssd_cache_load, self._layer(layer), slot.numel(), slot, k, v, ld,
+                   self._dtype(k), self.status)
         return k, v
 
     def _slots(self, slot: torch.Tensor, rows: int) -> None:
@@ -166,7 +171,7 @@ class PagedCache:
         nbytes = abi.ssd_cache_attention_workspace(cache, a)
         if self._workspace.numel() < nbytes:
             self._workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        abi.ssd_cache_attention(cache, a, self._workspace if nbytes else None, nbytes, self._stream())
+        self._call(abi.ssd_cache_attention, cache, a, self._workspace if nbytes else None, nbytes)
         return out
 
 

@@ -151,3 +151,27 @@ def test_contexts_with_an_8bit_cache(abi):
     rc = abi._lib.ssd_create(ctypes.byref(_dims(kvdtype=i8)), ctypes.byref(w), ctypes.byref(abi.ssd_kv(**good)), 256, 1 << 10,
                              None, ctypes.byref(ctx))
     assert rc == abi.SSD_ERR_CAPACITY
+
+
+@pytest.mark.parametrize("max_seq", [100, 300, 600, 1000, 3000, 20000])
+@pytest.mark.parametrize("batch,heads,d_head", [(1, 2, 64), (1, 32, 128), (8, 12, 64), (60, 4, 128)])
+def test_contexts_hold_every_pass_of_the_attention(abi, max_seq, batch, heads, d_head):
+    """An 8-bit context's workspace covers a pass's rows, their slots and the attention's partial
+    results for any rows a pass may have, beside what a float32 one has (up to its longest cache)."""
+    from tests.test_abi_cpu import _dims
+    page, prompt = 16, min(max_seq - 1, 2000)
+    pages = -(-max_seq // page)
+    kw = dict(n_heads=heads, d_head=d_head, d_model=heads * d_head, max_batch=batch, max_gamma=32, max_prompt=prompt,
+              page_size=page, max_seq=max_seq, max_pages=pages)
+    rows = max(prompt, 33)
+    cache = abi.ssd_cache(n_pages=4, n_heads=heads, page_size=page, d_head=d_head)
+    most = 0
+    for B in {1, 2, batch // 2, batch}:
+        for C in list(range(1, 70)) + [127, 129, 200, 255, 257, 500, 513, 1000, rows]:
+            if 1 <= B <= batch and C <= rows:
+                most = max(most, abi.ssd_cache_attention_workspace(cache, abi.ssd_cache_attn(
+                    B=B, rows=B * C, max_rows=C, max_len=max_seq, n_q_heads=heads, dtype=abi.SSD_F32, ldq=heads * d_head,
+                    ldo=heads * d_head, max_pages=pages)))
+    need = most + 2 * batch * rows * heads * d_head * 4 + batch * rows * 8
+    other = abi.ssd_workspace_bytes(_dims(**kw)) if max_seq <= 1024 else 0
+    assert abi.ssd_workspace_bytes(_dims(kvdtype=abi.SSD_I8, **kw)) - other >= need
