@@ -35,11 +35,15 @@ __device__ __forceinline__ V scalar_load(const V* p) {
 // again the operand layout of the weights in O^T = V^T P^T when its K index 8 g + i names key
 // 4 g + i % 4 of half i / 4, so neither scores nor weights cross lanes but for the maximum.  V is
 // read row by row, DH / 16 codes a lane, and its bytes turned to columns in registers.  A unit's
-// codes and scales are requested two units ahead of their use and its page-table entries three.  EVEN:
+// codes and scales are requested one unit ahead of their use and its page-table entries two (two and
+// three, with more registers: 32 heads over 32768 positions 59.0 us against 58.2).  EVEN:
 // pages hold a multiple of 16 positions, so a half lies in one page and its entry and scales are
 // scalars; else every key has its own, which cross lanes.  Each wave keeps its own reference, sum
 // and largest value scale; they meet in LDS once.
-// Bound: bytes of codes for long contexts, the chain lengths -> table -> codes for short ones.
+// Bound: for long contexts the bytes of the codes, which lie scattered in pieces of a page and head
+// (one token, 32 heads of 128 over 32768 positions: 269 MB in 58 us with the merge, 4.6 TB/s; 32
+// tokens, 8 cache heads, up to 4096 positions: 130 MB in 42 us); for short ones the chain lengths ->
+// table -> codes (70 positions: 5.4 us, of which an empty kernel takes 3.9).
 template <typename T, int DH, bool BIAS, bool EVEN, int AW>
 __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_attn_kernel(const CacheAttnArgs a, const int tiles,
                                                                                const int splits, const uint32_t ps_inv) {
@@ -82,6 +86,8 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
   const uint32_t k_off = n * DH + 16 * g, v_off = 4 * g * DH + n * (DH / 16);  // in a half of one page
   constexpr int NE = EVEN ? 2 : 1;  // entries of a unit a lane holds
   struct Entries { int page[NE]; };
+  // (pages of one position are never EVEN)
+  auto page_index = [&](int key) { return EVEN ? (int)__umulhi((uint32_t)key, ps_inv) : page_of(key, a.page_size, ps_inv); };
   // (No load depends on a branch, here and in `request`: the counts by which a wave waits for its
   // loads stay known, and it waits for no later one.)
   auto entries = [&](int x) {
@@ -89,7 +95,7 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
 #pragma unroll
     for (int h = 0; h < NE; ++h) {
       const int key = min(x * UNIT + (EVEN ? 16 * h : lane & 31), kend - 1);
-      const int32_t* p = table + page_of(key, a.page_size, ps_inv);
+      const int32_t* p = table + page_index(key);
       t.page[h] = EVEN ? scalar_load(p) : *p;
     }
     return t;
@@ -100,10 +106,10 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
       const int key = x * UNIT + (EVEN ? 16 * h : lane & 31), page = t.page[h];
       const bool in = x < x1 && key < kend, ok = in && page >= 0 && page < a.n_pages;
       bad_page |= in && !ok;
-      const size_t sc = (size_t)(ok ? page : 0) * a.n_heads + hk;
+      const uint32_t sc = (uint32_t)(ok ? page : 0) * a.n_heads + hk;  // (below 2^32, as the rows)
       u.ks[h] = EVEN ? scalar_load(a.k_scale + sc) : a.k_scale[sc];
       u.vs[h] = EVEN ? scalar_load(a.v_scale + sc) : a.v_scale[sc];
-      u.row[h] = ok ? (uint32_t)sc * a.page_size + (key - page_of(key, a.page_size, ps_inv) * a.page_size) : NO_ROW;
+      u.row[h] = ok ? sc * a.page_size + (key - page_index(key) * a.page_size) : NO_ROW;
     }
     // keys without a row read the pools' first rows: their scores are masked
     if constexpr (EVEN) {
@@ -152,12 +158,12 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
   f32x4_t o[NB];
 #pragma unroll
   for (int d = 0; d < NB; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  Unit<DH, EVEN> ua, ub, uc;  // in turn: one in work, the others on their way
+  Unit<DH, EVEN> ua, ub;  // in turn: one in work, the other on its way
 
-  // Unit x from `cur`; the wave's next but one on its way to `next`.
+  // Unit x from `cur`; the wave's next on its way to `next`.
   auto step = [&](const Unit<DH, EVEN>& cur, Unit<DH, EVEN>& next, int x) {
-    const Entries then = entries(x + 3 * AW);  // before the codes, for which it must not wait
-    request(next, x + 2 * AW, ahead);
+    const Entries then = entries(x + 2 * AW);  // before the codes, for which it must not wait
+    request(next, x + AW, ahead);
     ahead = then;
     const bool rows = EVEN ? cur.row[0] != NO_ROW && cur.row[NE - 1] != NO_ROW : __all(cur.row[0] != NO_ROW);
     const bool full = rows && x * UNIT + UNIT - 1 <= first;  // no key of it is masked
@@ -261,14 +267,12 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
     }
   };
   if (x0 + wave < x1) {
-    Entries then = entries(x0 + wave + AW);
+    const Entries then = entries(x0 + wave + AW);
     request(ua, x0 + wave, ahead);
-    ahead = entries(x0 + wave + 2 * AW);
-    request(ub, x0 + wave + AW, then);
-    for (int x = x0 + wave; x < x1; x += 3 * AW) {
-      step(ua, uc, x);
+    ahead = then;
+    for (int x = x0 + wave; x < x1; x += 2 * AW) {
+      step(ua, ub, x);
       if (x + AW < x1) step(ub, ua, x + AW);
-      if (x + 2 * AW < x1) step(uc, ub, x + 2 * AW);
     }
   }
   if (bad_page) atomicOr(a.status, SSD_DEV_BAD_PAGE);
