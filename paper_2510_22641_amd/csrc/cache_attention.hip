@@ -11,12 +11,10 @@ namespace {
 
 constexpr int UNIT = 32;  // keys a wave takes at once
 
-// What a wave needs of a unit before its products: codes as loaded, and scales.
-template <int DH, bool EVEN>
-struct Unit {
-  uint4 k[2][DH / 64];        // keys 16 h + lane % 16: 16 codes from 64 i + 16 g on
-  uint32_t v[DH / 64][8];     // keys 16 h + 4 g + e (8 = 4 h + e): DH / 16 codes from lane % 16 on
-  // EVEN: of the keys' halves, the same in every lane; else [0] of key lane % 32
+// Where a unit's keys are, and their scales.  EVEN: of its two halves, the same in every lane; else
+// [0] of key lane % 32.
+template <bool EVEN>
+struct Keys {
   float ks[EVEN ? 2 : 1], vs[EVEN ? 2 : 1];
   uint32_t row[EVEN ? 2 : 1];
 };
@@ -34,16 +32,17 @@ __device__ __forceinline__ V scalar_load(const V* p) {
 // operands agree); the scores land with lane (pair l % 16, keys 4 g + e of either half), which is
 // again the operand layout of the weights in O^T = V^T P^T when its K index 8 g + i names key
 // 4 g + i % 4 of half i / 4, so neither scores nor weights cross lanes but for the maximum.  V is
-// read row by row, DH / 16 codes a lane, and its bytes turned to columns in registers.  A unit's
-// codes and scales are requested one unit ahead of their use and its page-table entries two (two and
-// three, with more registers: 32 heads over 32768 positions 59.0 us against 58.2).  EVEN:
+// read row by row, DH / 16 codes a lane, and its bytes turned to columns in registers.  The next
+// unit's codes are requested into the registers that this one's have just left, a whole unit before
+// their use; its scales one unit ahead and its page-table entries two (codes of a second or third
+// unit on their way in registers of their own measured 2 and 3% slower).  EVEN:
 // pages hold a multiple of 16 positions, so a half lies in one page and its entry and scales are
 // scalars; else every key has its own, which cross lanes.  Each wave keeps its own reference, sum
 // and largest value scale; they meet in LDS once.
 // Bound: for long contexts the bytes of the codes, which lie scattered in pieces of a page and head
-// (one token, 32 heads of 128 over 32768 positions: 269 MB in 58 us with the merge, 4.6 TB/s; 32
-// tokens, 8 cache heads, up to 4096 positions: 130 MB in 42 us); for short ones the chain lengths ->
-// table -> codes (70 positions: 5.4 us, of which an empty kernel takes 3.9).
+// (one token, 32 heads of 128 over 32768 positions: 269 MB in 52 us and 5 for the merge; 32 tokens of
+// 2048 positions, 8 cache heads: 134 MB in 33 us; of 1 to 4096: 130 MB in 41); for short ones the
+// chain lengths -> table -> codes (70 positions: 5.4 us, of which an empty kernel takes 3.9).
 template <typename T, int DH, bool BIAS, bool EVEN, int AW>
 __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_attn_kernel(const CacheAttnArgs a, const int tiles,
                                                                                const int splits, const uint32_t ps_inv) {
@@ -100,7 +99,7 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
     }
     return t;
   };
-  auto request = [&](Unit<DH, EVEN>& u, int x, const Entries& t) {
+  auto locate = [&](Keys<EVEN>& u, int x, const Entries& t) {
 #pragma unroll
     for (int h = 0; h < NE; ++h) {
       const int key = x * UNIT + (EVEN ? 16 * h : lane & 31), page = t.page[h];
@@ -111,38 +110,33 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
       u.vs[h] = EVEN ? scalar_load(a.v_scale + sc) : a.v_scale[sc];
       u.row[h] = ok ? sc * a.page_size + (key - page_index(key) * a.page_size) : NO_ROW;
     }
-    // keys without a row read the pools' first rows: their scores are masked
-    if constexpr (EVEN) {
+  };
+  // Codes as loaded: of keys 16 h + lane % 16, 16 from 64 i + 16 g on; and of keys 16 h + 4 g + e
+  // (8 = 4 h + e), DH / 16 from lane % 16 on.  Keys without a row read the pools' first rows: their
+  // scores are masked.
+  uint4 kc[2][DH / 64];
+  uint32_t vc[VW][8];
+  auto first_byte = [&](const Keys<EVEN>& u, int h, int key) -> size_t {  // of a key of half h
+    const uint32_t r = EVEN ? u.row[h % NE] : (uint32_t)__shfl(u.row[0], 16 * h + key, SSD_WAVE);
+    return (size_t)(r == NO_ROW ? 0 : r) * DH;
+  };
+  auto request_k = [&](const Keys<EVEN>& u) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const size_t at = (size_t)(u.row[h] == NO_ROW ? 0 : u.row[h]) * DH;
-        const int8_t* kb = a.k_codes + at;
-        const int8_t* vb = a.v_codes + at;
+    for (int h = 0; h < 2; ++h) {
+      const int8_t* p = a.k_codes + first_byte(u, h, n) + (EVEN ? k_off : 16 * g);
 #pragma unroll
-        for (int i = 0; i < DH / 64; ++i) u.k[h][i] = *reinterpret_cast<const uint4*>(kb + k_off + 64 * i);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-#pragma unroll
-          for (int i = 0; i < VW; ++i) u.v[i][4 * h + e] = *reinterpret_cast<const uint32_t*>(vb + v_off + e * DH + 4 * i);
-      }
-    } else {
-      auto at = [&](int key) -> size_t {
-        const uint32_t r = __shfl(u.row[0], key, SSD_WAVE);
-        return (size_t)(r == NO_ROW ? 0 : r) * DH;
-      };
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const uint4* pk = reinterpret_cast<const uint4*>(a.k_codes + at(16 * h + n) + 16 * g);
-#pragma unroll
-        for (int i = 0; i < DH / 64; ++i) u.k[h][i] = pk[4 * i];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t* pv = reinterpret_cast<const uint32_t*>(a.v_codes + at(16 * h + 4 * g + e) + n * (DH / 16));
-#pragma unroll
-          for (int i = 0; i < VW; ++i) u.v[i][4 * h + e] = pv[i];
-        }
-      }
+      for (int i = 0; i < DH / 64; ++i) kc[h][i] = *reinterpret_cast<const uint4*>(p + 64 * i);
     }
+  };
+  auto request_v = [&](const Keys<EVEN>& u) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int8_t* p = a.v_codes + first_byte(u, h, 4 * g + e) + (EVEN ? v_off + e * DH : n * (DH / 16));
+#pragma unroll
+        for (int i = 0; i < VW; ++i) vc[i][4 * h + e] = *reinterpret_cast<const uint32_t*>(p + 4 * i);
+      }
   };
 
   // (the first unit's entries before the queries: neither waits for the other)
@@ -158,21 +152,29 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
   f32x4_t o[NB];
 #pragma unroll
   for (int d = 0; d < NB; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  Unit<DH, EVEN> ua, ub;  // in turn: one in work, the other on its way
+  Keys<EVEN> cur = {}, next;
+  float bias[8];
+  auto request_bias = [&](int x) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      bias[i] = bias_row[max(0, min(pos - (x * UNIT + 16 * (i / 4) + 4 * g + i % 4), a.n_bias - 1))];
+  };
 
-  // Unit x from `cur`; the wave's next on its way to `next`.
-  auto step = [&](const Unit<DH, EVEN>& cur, Unit<DH, EVEN>& next, int x) {
+  if (x0 + wave < x1) {
+    const Entries then = entries(x0 + wave + AW);
+    locate(cur, x0 + wave, ahead);
+    if constexpr (BIAS) request_bias(x0 + wave);
+    request_k(cur);
+    request_v(cur);
+    ahead = then;
+  }
+  // The next unit's codes are requested as soon as this one's have left their registers.
+  for (int x = x0 + wave; x < x1; x += AW, cur = next) {
     const Entries then = entries(x + 2 * AW);  // before the codes, for which it must not wait
-    request(next, x + AW, ahead);
+    locate(next, x + AW, ahead);
     ahead = then;
     const bool rows = EVEN ? cur.row[0] != NO_ROW && cur.row[NE - 1] != NO_ROW : __all(cur.row[0] != NO_ROW);
     const bool full = rows && x * UNIT + UNIT - 1 <= first;  // no key of it is masked
-    float bias[8];
-    if constexpr (BIAS) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        bias[i] = bias_row[max(0, min(pos - (x * UNIT + 16 * (i / 4) + 4 * g + i % 4), a.n_bias - 1))];
-    }
     // scales over the unit's largest
     float ks[NE], vs[NE];
 #pragma unroll
@@ -197,7 +199,7 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
       const float k = (EVEN ? ks[h % NE] : __shfl(ks[0], 16 * h + n, SSD_WAVE)) * kinv;
       const Ratio kr = ratio_of(k, k);
       s[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      const uint32_t* kw = reinterpret_cast<const uint32_t*>(&cur.k[h][0]);
+      const uint32_t* kw = reinterpret_cast<const uint32_t*>(&kc[h][0]);
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
         const f16x8_t kf = codes8(kw[2 * st], kw[2 * st + 1], kr);
@@ -210,6 +212,10 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[i / 4][i % 4] = fmaf(s[i / 4][i % 4], f, bias[i]);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (BIAS) request_bias(x + AW);
+    request_k(next);
+    __builtin_amdgcn_sched_barrier(0);
     if (!full) {  // (uniform)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -258,22 +264,16 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
 #pragma unroll
     for (int i = 0; i < VW; ++i) {
       f16x8_t vf[4];
-      columns4(cur.v[i], vr, vf);
+      columns4(vc[i], vr, vf);
 #pragma unroll
       for (int d = 0; d < 4; ++d)
 #pragma unroll
         for (int p = NP - 1; p >= 0; --p)
           o[4 * i + d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[d], pf[p], o[4 * i + d], 0, 0, 0);
     }
-  };
-  if (x0 + wave < x1) {
-    const Entries then = entries(x0 + wave + AW);
-    request(ua, x0 + wave, ahead);
-    ahead = then;
-    for (int x = x0 + wave; x < x1; x += 2 * AW) {
-      step(ua, ub, x);
-      if (x + AW < x1) step(ub, ua, x + AW);
-    }
+    __builtin_amdgcn_sched_barrier(0);
+    request_v(next);
+    __builtin_amdgcn_sched_barrier(0);
   }
   if (bad_page) atomicOr(a.status, SSD_DEV_BAD_PAGE);
   const float back = vref * (1.f / W_TOP);
@@ -422,8 +422,8 @@ hipError_t launch_t(const CacheAttnArgs& a, hipStream_t s) {
 
 // Key ranges a (row, head) pair's keys are split into: a block for each of the 256 compute units (two
 // of the 64-pair kernel's four waves), while a range keeps 128 keys.  More of them measured no
-// faster (one token of 32 heads over 32768 positions: 58 us with 256 blocks of eight waves, 64 with
-// 512; 32 tokens of 8 cache heads: 43 against 50).  The few-row kernel keeps short ranges whole, where
+// faster (one token of 32 heads over 32768 positions: 57 us with 256 blocks of eight waves, 60 with
+// 512; 32 tokens of 8 cache heads: 41 against 47).  The few-row kernel keeps short ranges whole, where
 // the merge would cost more than the waves save (one token of 32 heads of 128: 300 positions 8.7 us
 // whole, 9.6 in three ranges; 1000: 13.6 and 9.7 in eight; four tokens, 1000: 15.1 and 16.1 in two).
 int cache_attn_splits(const CacheAttnArgs& a) {
