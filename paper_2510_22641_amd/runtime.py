@@ -61,7 +61,7 @@ class PagedCache:
         self.seq_len = torch.zeros(max_batch, dtype=torch.int32, device=self.device)
         self.taken = torch.zeros(1, dtype=torch.int32, device=self.device)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
-        self._workspace = torch.empty(0, dtype=torch.uint8, device=self.device)
+        self.device = self.seq_len.device  # "cuda" is the device of today, whichever is current later
 
     def _call(self, fn, *args):
         """A library call on torch's current stream of the device (its null stream is the current
@@ -169,9 +169,9 @@ class PagedCache:
                                status=self.status)
         cache = self._layer(layer)
         nbytes = abi.ssd_cache_attention_workspace(cache, a)
-        if self._workspace.numel() < nbytes:
-            self._workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-        self._call(abi.ssd_cache_attention, cache, a, self._workspace if nbytes else None, nbytes)
+        # (a workspace of its own for each call: calls on several streams and captured ones share none)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
+        self._call(abi.ssd_cache_attention, cache, a, ws, nbytes)
         return out
 
 

@@ -632,3 +632,31 @@ def test_a_captured_step_replays():
         ref, tol = attend_reference(c, 0, q, [n[0] - 1, n[1] - 1], [1, 1], 0.125)
         assert bool(((got.double().cpu() - ref).abs() <= tol).all()) and int(st) == 0
         lens += 1
+
+
+def test_a_captured_call_keeps_its_workspace():
+    """A captured call and the calls after it, larger ones and others' tensors among them, do not write
+    each other's memory."""
+    runtime, _ = _mods()
+    c, g = make_cache([2000, 900], heads=2, max_seq=2048)
+    assert c.device.index is not None
+    q = torch.randn(2, 4, 64, generator=g).cuda()
+    first, _ = c.grow([1, 1])
+    c.attend(0, q, first, 1, 0.125)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        out = c.attend(0, q, first, 1, 0.125)
+    rs, _ = c.grow([9, 30])
+    more = torch.randn(39, 4, 64, generator=g).cuda()
+    late = c.attend(0, more, rs, 30, 0.125)
+    ones = [torch.ones(1 << n, device="cuda") for n in range(8, 19) for _ in range(3)]
+    # (a row sits at its sequence's end, which has moved)
+    ref, tol = attend_reference(c, 0, q, [n - 1 for n in c.lens], [1, 1], 0.125)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert bool(((out.double().cpu() - ref).abs() <= tol).all())
+        assert all(bool((t == 1).all()) for t in ones)
+        assert torch.equal(late, c.attend(0, more, rs, 30, 0.125)) and int(c.status) == 0
