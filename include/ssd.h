@@ -369,7 +369,7 @@ typedef struct {
   void* v_codes;     /* same */
   float* k_scale;    /* [n_pages][n_heads] */
   float* v_scale;    /* same */
-  int32_t n_pages;
+  int32_t n_pages;   /* n_pages * n_heads * page_size < 2^32 - 1 */
   int32_t n_heads;   /* heads of the cache; the queries may have a multiple of them */
   int32_t page_size; /* 1 .. 256 positions */
   int32_t d_head;    /* 64 or 128 */
