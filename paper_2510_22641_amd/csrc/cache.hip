@@ -140,19 +140,13 @@ __global__ __launch_bounds__(MAP_THREADS) void page_map_kernel(const PageMapArgs
         const int i = page_of((int)p, a.page_size, ps_inv);
         int first;
         const int n = need(len, row0[b + 1] - row0[b], first);
-        int page;
-        if (a.free_pages && i >= first && n > 0) {
-          const int t = page0[b] + i - first;
-          page = t < page0[b + 1] ? a.free_pages[t] : -1;
-        } else {
-          page = a.page_table[(size_t)b * a.max_pages + i];
-          if (page < 0) atomicOr(a.status, SSD_DEV_BAD_PAGE);
+        const bool is_new = a.free_pages && i >= first && n > 0;
+        const int t = page0[b] + i - first;
+        if (!is_new || t < page0[b + 1]) {  // else the free list has ended
+          const int page = is_new ? a.free_pages[t] : a.page_table[(size_t)b * a.max_pages + i];
+          if (page < 0 || page >= a.n_pages) atomicOr(a.status, SSD_DEV_BAD_PAGE);
+          else s = (int64_t)page * a.page_size + ((int)p - i * a.page_size);
         }
-        if (page >= a.n_pages) {
-          atomicOr(a.status, SSD_DEV_BAD_PAGE);
-          page = -1;
-        }
-        if (page >= 0) s = (int64_t)page * a.page_size + ((int)p - i * a.page_size);
       }
     }
     a.slot[r] = s;
@@ -239,7 +233,7 @@ constexpr int STORE_HELD = 8;  // passes of rows kept in registers between the m
 // run's codes; 32 (or 16) lanes take four elements each of a row.  Every block belongs to one wave,
 // so nothing is atomic.  Bound: bytes for long prompts (8192 bf16 rows of 32 heads of 128, K and V:
 // 201 MB in 49 us, 4.1 TB/s, where a large copy reaches 4.9); the chain slot -> rows, codes and
-// scale -> reduction -> store for single tokens (32 of 12 heads of 64: 5.0 us).
+// scale -> reduction -> store for single tokens (29 float32 rows of 32 heads of 64: 5.0 us).
 template <typename T, int DH, bool VEC>
 __global__ __launch_bounds__(64 * STORE_WAVES) void cache_store_kernel(const CacheRowsArgs a, const int window,
                                                                        const int groups, const double ps_inv) {

@@ -200,6 +200,14 @@ def test_page_map_reports_what_does_not_fit():
     assert slot[0] == -1 and slot[1] == -1 and st & abi.SSD_DEV_BAD_PAGE
 
 
+@pytest.mark.parametrize("free", [-1, -5, 10, 2 ** 31 - 1])
+def test_page_map_reports_pages_outside_in_the_free_list(free):
+    _, abi = _mods()
+    t, rs, slot, taken, st = _map(abi, [1, 0], [1, 3], [4, free], [[2, -1], [-1, -1]], 2, 10, 4)
+    assert (t, rs, taken) == ([[2, -1], [4, free]], [0, 1, 4], 2)
+    assert slot == [5, 8, 9, -1] and st == abi.SSD_DEV_BAD_PAGE
+
+
 # ---- stored rows --------------------------------------------------------------------------------
 
 
