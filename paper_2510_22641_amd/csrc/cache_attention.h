@@ -194,6 +194,21 @@ __device__ __forceinline__ void store_out(T* o, const float* f, bool vec) {
   }
 }
 
+// N (a multiple of 4) consecutive outputs of row `row` from dimension d of head `head` on.
+template <typename T, int DH, int N>
+__device__ __forceinline__ void store_result(const CacheAttnArgs& a, size_t row, size_t head, int d, const float* f) {
+  if constexpr (sizeof(T) == 4) {
+    if (a.out_planes) {
+#pragma unroll
+      for (int i = 0; i < N; i += 4)
+        store_planes4(a.out_planes + plane_at((int)row, (int)head * DH + d + i, (a.rows + 15) >> 4), f[i], f[i + 1],
+                      f[i + 2], f[i + 3]);
+      return;
+    }
+  }
+  store_out<T, N>(reinterpret_cast<T*>(a.out) + row * a.ldo + head * DH + d, f, a.out_vec);
+}
+
 // No row: what a key outside the sequence or on a page outside the pools has for its row of codes.
 // (Row (page n_heads + head) page_size + offset of the pools; there are fewer than 2^32 of them.)
 constexpr uint32_t NO_ROW = 0xffffffffu;

@@ -320,7 +320,7 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
   const float inv = L == 0.f ? 0.f : 1.f / L;  // (NaN stays)
 #pragma unroll
   for (int i = 0; i < PART; ++i) f[i] *= inv;
-  store_out<T, PART>(reinterpret_cast<T*>(a.out) + row * a.ldo + (size_t)ph * DH + d0, f, a.out_vec);
+  store_result<T, DH, PART>(a, row, ph, d0, f);
 }
 
 // The splits' results of row blockIdx.y of sequence blockIdx.z and one head: per pair `splits` rows
@@ -363,7 +363,10 @@ __global__ __launch_bounds__(MERGE) void cache_attn_merge_kernel(const CacheAttn
 #pragma unroll
     for (int k = 0; k < GROUPS; ++k) v += xo[k][tid];
     const float inv = L == 0.f ? 0.f : 1.f / L;
-    store_elem(reinterpret_cast<T*>(a.out) + (size_t)r * a.ldo + (size_t)h * DH + tid, v * inv);
+    if (sizeof(T) == 4 && a.out_planes)
+      store_planes1(a.out_planes + plane_at(r, h * DH + tid, (a.rows + 15) >> 4), v * inv);
+    else
+      store_elem(reinterpret_cast<T*>(a.out) + (size_t)r * a.ldo + (size_t)h * DH + tid, v * inv);
   }
 }
 

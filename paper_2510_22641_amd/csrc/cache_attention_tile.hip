@@ -343,7 +343,7 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
         p[(size_t)splits * DH + 2 * split + 1] = L;
       }
     } else {
-      store_out<T, DH / 4>(reinterpret_cast<T*>(a.out) + row * a.ldo + head * DH + g * (DH / 4), f, a.out_vec);
+      store_result<T, DH, DH / 4>(a, row, head, g * (DH / 4), f);
     }
   }
 }

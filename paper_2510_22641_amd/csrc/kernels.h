@@ -423,6 +423,8 @@ struct CacheAttnArgs {
   void* out;
   int64_t ldo;
   bool out_vec;              // rows of out are aligned for four elements a store
+  // optional: float32 rows go here instead, as hi / lo planes in fragment order
+  bf16_t* out_planes = nullptr;
   const int32_t* row_start;  // [B + 1], or null: max_rows rows each
   const int32_t* seq_len;
   int pos_off;

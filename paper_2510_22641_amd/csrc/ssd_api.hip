@@ -114,7 +114,7 @@ bool make_layout(const ssd_dims& d, Layout& L, bool allow_fold = true, bool allo
     L.x = take(R * D * 4);
     L.x1 = take((B * D + HD) * 4);  // room for a one-row attention output right after the row
     L.q = take(R * HD * 4);
-    L.attn = take((i8 ? R : R1) * HD * 4);
+    L.attn = take(R1 * HD * 4);
     L.ffn = take(R1 * (size_t)d.d_ff * 4);
     L.inh = take(B * (size_t)d.in_hidden * 4);
     L.xi = take(B * D * 4);
@@ -358,7 +358,7 @@ int pass_slots(ssd_ctx* c, int B, int C, int pos_off) {
 
 // Self-attention of a pass over an 8-bit cache: the projection's rows into the blocks, then the
 // queries over them.
-int attend_i8(ssd_ctx* c, int l, int B, int C, int pos_off, const float* q, float* out) {
+int attend_i8(ssd_ctx* c, int l, int B, int C, int pos_off, const float* q, float* out, bf16_t* out_planes) {
   const ssd_dims& d = c->d;
   const bool t5 = d.arch == SSD_ARCH_T5;
   const int HD = d.n_heads * d.d_head;
@@ -376,7 +376,7 @@ int attend_i8(ssd_ctx* c, int l, int B, int C, int pos_off, const float* q, floa
   CacheAttnArgs a = cache_attn_of(d, B, C);
   a.k_codes = k_codes; a.v_codes = v_codes; a.k_scale = r.k_scale; a.v_scale = r.v_scale;
   a.n_pages = c->kv.n_pages;
-  a.q = q; a.ldq = HD; a.out = out; a.ldo = HD; a.out_vec = true;
+  a.q = q; a.ldq = HD; a.out = out; a.ldo = HD; a.out_vec = true; a.out_planes = out_planes;
   a.seq_len = c->kv.seq_len; a.pos_off = pos_off; a.page_table = c->kv.page_table;
   a.bias = t5 ? c->at<float>(c->L.bias_tab) : nullptr; a.n_bias = d.max_seq;
   a.scale = t5 ? 1.0f : (float)(1.0 / std::sqrt((double)d.d_head));
@@ -452,10 +452,8 @@ int run_layers(ssd_ctx* c, float* x, int B, int C, int pos_off, int l0, int l1, 
     at.scale = t5 ? 1.0f : (float)(1.0 / std::sqrt((double)d.d_head));
     at.status = status;
     if (i8) {
-      float* out = fg ? x + D : attn;
-      const int rc = attend_i8(c, l, B, C, pos_off, q, out);
+      const int rc = attend_i8(c, l, B, C, pos_off, q, (float*)at.out, at.out_planes);
       if (rc) return rc;
-      if (planes) HIP_TRY(launch_rows_prep(out, HD, R, HD, nullptr, nullptr, 0.f, p_attn, nullptr, s));
     } else {
       HIP_TRY(launch_attention(at, s));
     }
