@@ -1,14 +1,18 @@
 // Device helpers shared by the kernels of attention over the 8-bit paged cache.
 //
-// Codes are whole numbers below 2^7 and scales powers of two, so a code times the ratio of its scale
-// to the largest one of the keys it is worked on with is exact in f16 down to ratios of 2^-24, and
-// the products run on the f16 matrix instruction.  Queries enter scaled by a power of two that puts
+// Codes are whole numbers below 2^7 and scales powers of two, so a code times the ratio of its key's
+// scale to the largest one of the keys it is worked on with is exact in f16 down to ratios of 2^-24,
+// and the products run on the f16 matrix instruction.  Queries enter scaled by a power of two that puts
 // their row's largest element into [2^14, 2^15): bf16 ones as one f16 plane (11 bits against
 // their 8), float32 ones as two (22 bits: an element is off by at most 2^-23 of itself, less than a
-// sum of 64 products in float32 loses).  Weights are one plane for bf16 rows (2^-11, an eighth of
-// the output's own rounding) and two for float32, W_TOP times their value: the reference that the
-// softmax subtracts follows the running maximum in steps of at least REF_STEP, so they stay under
-// 2^15, and those under 2^-21 of the reference's are off by 2^-32 of it.
+// sum of 64 products in float32 loses).
+//
+// Weights enter the second product times their key's value scale, under a power of two of the
+// row's own that follows the largest such product (struct Reference): a key counts there by what it
+// adds to the output, so a block of large values with no weight, or one that the row may not attend,
+// takes no bits from the others.  They are one plane for bf16 rows (2^-11, an eighth of the
+// output's own rounding) and two for float32, between 2^W_EXP and 2^(W_EXP + REF_STEP) for the
+// largest; those under f16's normal numbers are off by 2^-25, 2^-32 of the largest.
 #pragma once
 
 #include "device.h"
@@ -23,8 +27,9 @@ typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr float LOG2E = 1.4426950408889634f;
-constexpr float W_TOP = 128.f;   // weights' scale
+constexpr int W_EXP = 7;         // exponent of the weights' scale
 constexpr float REF_STEP = 8.f;  // in powers of two
+constexpr int NO_EXP = -10000;   // exponent of a scale of 0, whose block has not been written
 
 template <typename T> struct Planes { static constexpr int N = sizeof(T) == 4 ? 2 : 1; };
 
@@ -55,6 +60,12 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t w_flipped, uint32_t sel, 
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(v, t.r, t.off));
 }
 
+// The codes themselves.
+__device__ __forceinline__ uint32_t code_pair(uint32_t w_flipped, uint32_t sel) {
+  const f16x2_t v = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, w_flipped, sel));
+  return __builtin_bit_cast(uint32_t, v - f16x2_t{(_Float16)1152.f, (_Float16)1152.f});
+}
+
 // Eight consecutive codes of a key's row.
 __device__ __forceinline__ f16x8_t codes8(uint32_t a, uint32_t b, const Ratio& t) {
   a ^= 0x80808080u;
@@ -63,17 +74,19 @@ __device__ __forceinline__ f16x8_t codes8(uint32_t a, uint32_t b, const Ratio& t
                   code_pair(b, 0x04030402, t));
 }
 
-// Eight keys' dwords, four dimensions each: operand d is dimension d of the eight keys.
-__device__ __forceinline__ void columns4(const uint32_t (&w)[8], const Ratio (&t)[4], f16x8_t (&out)[4]) {
+// Eight keys' dwords, four dimensions each: operand d is dimension d of the eight keys, by code_pair's
+// last arguments t[k] of keys 2 k and 2 k + 1.
+template <typename... R>
+__device__ __forceinline__ void columns4(const uint32_t (&w)[8], f16x8_t (&out)[4], const R (&... t)[4]) {
   uint32_t p[4][4];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const uint32_t a = w[2 * k] ^ 0x80808080u, b = w[2 * k + 1] ^ 0x80808080u;
     const uint32_t x = __builtin_amdgcn_perm(b, a, 0x05010400), y = __builtin_amdgcn_perm(b, a, 0x07030602);
-    p[0][k] = code_pair(x, 0x04010400, t[k]);
-    p[1][k] = code_pair(x, 0x04030402, t[k]);
-    p[2][k] = code_pair(y, 0x04010400, t[k]);
-    p[3][k] = code_pair(y, 0x04030402, t[k]);
+    p[0][k] = code_pair(x, 0x04010400, t[k]...);
+    p[1][k] = code_pair(x, 0x04030402, t[k]...);
+    p[2][k] = code_pair(y, 0x04010400, t[k]...);
+    p[3][k] = code_pair(y, 0x04030402, t[k]...);
   }
 #pragma unroll
   for (int d = 0; d < 4; ++d) out[d] = f16_frag(p[d][0], p[d][1], p[d][2], p[d][3]);
@@ -82,15 +95,11 @@ __device__ __forceinline__ void columns4(const uint32_t (&w)[8], const Ratio (&t
 // A scale's power of two (0 where no block has been written), its exponent and its reciprocal (a
 // large number for 0, whose blocks' ratios are 0 all the same).
 __device__ __forceinline__ float pow2_of(float s) { return __uint_as_float(__float_as_uint(s) & 0x7f800000u); }
-__device__ __forceinline__ int exp_of(float p) { return (int)(__float_as_uint(p) >> 23) - 127; }
-__device__ __forceinline__ float pow2_inv(float p) { return __uint_as_float(0x7f000000u - __float_as_uint(p)); }
-
-// Factor of a unit's weights: W_TOP times its largest value scale over the largest so far, as an
-// exponent.  (Under 2^-60 the weights are nothing in f16; the bound keeps the sum's own scale finite.)
-__device__ __forceinline__ int weight_exp(float vtop, float vref) {
-  const int e = exp_of(W_TOP) + exp_of(vtop) - exp_of(vref);
-  return e < -60 ? -60 : e;
+__device__ __forceinline__ int exp_of(float s) {
+  const int e = (int)(__float_as_uint(s) >> 23 & 0xff);
+  return e ? e - 127 : NO_EXP;
 }
+__device__ __forceinline__ float pow2_inv(float p) { return __uint_as_float(0x7f000000u - __float_as_uint(p)); }
 
 // The factor of a row's products over keys of largest key scale ktop.
 __device__ __forceinline__ float score_factor(float qf, float ktop) {
@@ -213,25 +222,34 @@ __device__ __forceinline__ void store_result(const CacheAttnArgs& a, size_t row,
 // (Row (page n_heads + head) page_size + offset of the pools; there are fewer than 2^32 of them.)
 constexpr uint32_t NO_ROW = 0xffffffffu;
 
-// The running reference of a row's softmax.  Scores are t = s * f (+ bias); without a bias f carries
+// Value scales of keys that one exponent serves differ by at most this many powers of two.
+constexpr int NEAR = 4;
+
+// The running references of a row's softmax.  Scores are t = s * f (+ bias); without a bias f carries
 // log2 e and t is in powers of two, with one t stays in natural units, where the type's lowest value
-// is a finite number (times log2 e it would not be).
+// is a finite number (times log2 e it would not be).  The weights e^(t - ref) sum up to the
+// denominator; the second product takes them times 2^(value exponent + W_EXP - num).  Both begin
+// below what any key has: the lowest value is its own reference, and -inf stays under it.
 template <bool BIAS>
 struct Reference {
-  float ref = -INFINITY;  // subtracted from the scores; -inf before the first key
+  static constexpr float UNIT = BIAS ? LOG2E : 1.f;  // of t, in powers of two
+  float ref = -FLT_MAX;      // subtracted from the scores
+  float num = 2.f * NO_EXP;  // a whole number of powers of two beside it, the numerator's
 
-  // Takes in the largest score of new keys (the same in the row's four lanes); whether any row of
-  // the wave moves, and then by what its sums shrink.
-  __device__ __forceinline__ bool move(float top, float& drop) {
-    constexpr float step = BIAS ? REF_STEP / LOG2E : REF_STEP;
-    drop = 1.f;
-    if (!__any(top > ref + step)) return false;  // (-inf + step is -inf)
-    const float next = fmaxf(ref, top);
-    drop = __builtin_amdgcn_exp2f((ref - (next == -INFINITY ? 0.f : next)) * (BIAS ? LOG2E : 1.f));
+  // Takes in new keys: `top`, their largest score, and `e`, the largest of their scores less top plus
+  // the value exponents, in powers of two, or up to NEAR more (both the same in the row's four
+  // lanes).  Whether any row of the wave moves, and then by what its sums shrink.
+  __device__ __forceinline__ bool move(float top, float e, float& drop, float& num_drop) {
+    drop = num_drop = 1.f;
+    if (!__any(top - ref > fminf(REF_STEP / UNIT, (num + REF_STEP - e) * (1.f / UNIT)))) return false;
+    const float next = fmaxf(ref, top), shift = (ref - next) * UNIT;
+    const float n = ceilf(fmaxf(num + shift, fmaf(top - next, UNIT, e)));
+    drop = __builtin_amdgcn_exp2f(shift);
+    num_drop = __builtin_amdgcn_exp2f(num - n + shift);
     ref = next;
+    num = n;
     return true;
   }
-  __device__ __forceinline__ float used() const { return ref == -INFINITY ? 0.f : ref; }  // weights of zero
 };
 
 }  // namespace ssd

@@ -37,8 +37,9 @@ __device__ __forceinline__ V scalar_load(const V* p) {
 // their use; its scales one unit ahead and its page-table entries two (codes of a second or third
 // unit on their way in registers of their own measured 2 and 3% slower).  EVEN:
 // pages hold a multiple of 16 positions, so a half lies in one page and its entry and scales are
-// scalars; else every key has its own, which cross lanes.  Each wave keeps its own reference, sum
-// and largest value scale; they meet in LDS once.
+// scalars; else every key has its own, which cross lanes.  The codes of V are operands as they are;
+// their scales multiply the weights.  Each wave keeps its own references and sums; they meet in LDS
+// once.
 // Bound: for long contexts the bytes of the codes, which lie scattered in pieces of a page and head
 // (one token, 32 heads of 128 over 32768 positions: 269 MB in 52 us and 5 for the merge; 32 tokens of
 // 2048 positions, 8 cache heads: 134 MB in 33 us; of 1 to 4096: 130 MB in 41); for short ones the
@@ -50,7 +51,7 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
   constexpr int NB = DH / 16;  // output blocks of 16 dimensions
   constexpr int VW = DH / 64;  // dwords of V a lane and key
   constexpr int NP = Planes<T>::N;
-  constexpr bool EXACT = BIAS || sizeof(T) == 4;  // weights from the scores' differences alone
+  constexpr bool EXACT = BIAS || sizeof(T) == 4 || !EVEN;  // weights from the scores' differences alone
   __shared__ float xo[AW][16][DH + 4];
   __shared__ float xm[AW][16], xl[AW][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -148,7 +149,7 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
                                      a.scale, q) * (BIAS ? 1.f : LOG2E);
   const float* bias_row = BIAS ? a.bias + (size_t)hq * a.n_bias : nullptr;
   Reference<BIAS> ref;
-  float l = 0.f, vref = 0.f;  // sum of the weights; largest value scale so far
+  float l = 0.f;  // sum of the weights
   f32x4_t o[NB];
 #pragma unroll
   for (int d = 0; d < NB; ++d) o[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -175,24 +176,24 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
     ahead = then;
     const bool rows = EVEN ? cur.row[0] != NO_ROW && cur.row[NE - 1] != NO_ROW : __all(cur.row[0] != NO_ROW);
     const bool full = rows && x * UNIT + UNIT - 1 <= first;  // no key of it is masked
-    // scales over the unit's largest
-    float ks[NE], vs[NE];
+    // key scales over the unit's largest, exponents of the value scales: of the halves, or the lane's keys
+    float ks[NE];
+    int ve[EVEN ? 2 : 8];
 #pragma unroll
     for (int h = 0; h < NE; ++h) {
       ks[h] = cur.row[h] != NO_ROW ? cur.ks[h] : 0.f;
-      vs[h] = cur.row[h] != NO_ROW ? cur.vs[h] : 0.f;
+      ve[h] = cur.row[h] != NO_ROW ? exp_of(cur.vs[h]) : NO_EXP;
     }
-    float ktop = fmaxf(ks[0], ks[NE - 1]), vtop = fmaxf(vs[0], vs[NE - 1]);
+    float ktop = fmaxf(ks[0], ks[NE - 1]);
     if constexpr (!EVEN) {
 #pragma unroll
-      for (int i = 1; i < 32; i <<= 1) {
-        ktop = fmaxf(ktop, __shfl_xor(ktop, i, SSD_WAVE));
-        vtop = fmaxf(vtop, __shfl_xor(vtop, i, SSD_WAVE));
-      }
+      for (int i = 1; i < 32; i <<= 1) ktop = fmaxf(ktop, __shfl_xor(ktop, i, SSD_WAVE));
+      const int own = ve[0];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ve[i] = __shfl(own, 16 * (i / 4) + 4 * g + i % 4, SSD_WAVE);
     }
     ktop = pow2_of(ktop);
-    vtop = pow2_of(vtop);
-    const float kinv = pow2_inv(ktop), vinv = pow2_inv(vtop);
+    const float kinv = pow2_inv(ktop);
     f32x4_t s[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -224,47 +225,62 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
         if (row == NO_ROW || x * UNIT + src > pos) s[i / 4][i % 4] = -INFINITY;
       }
     }
-    float mx = max3(max3(s[0][0], s[0][1], s[0][2]), max3(s[0][3], s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]));
-    mx = col_max(mx) * (BIAS ? 1.f : f);
-    float drop, vdrop = 1.f;
-    bool shrink = ref.move(mx, drop);
-    if (vtop > vref) {
-      vdrop = vref * vinv;
-      vref = vtop;
-      shrink = true;
+    const float c = BIAS ? 1.f : f;
+    auto half_max = [&](int h) { return max3(max3(s[h][0], s[h][1], s[h][2]), s[h][3], s[h][3]); };
+    const float mx = col_max(max3(half_max(0), half_max(1), half_max(1))) * c;
+    float ex;
+    if constexpr (EVEN) {
+      ex = (float)max(ve[0], ve[1]);
+      if (abs(ve[0] - ve[1]) > NEAR)  // (uniform)
+        ex = fmaxf(fmaf(col_max(half_max(0)) * c - mx, ref.UNIT, (float)ve[0]),
+                   fmaf(col_max(half_max(1)) * c - mx, ref.UNIT, (float)ve[1]));
+    } else {
+      ex = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ex = fmaxf(ex, fmaf(s[i / 4][i % 4] * c - mx, ref.UNIT, (float)ve[i]));
+      ex = col_max(ex);
     }
-    if (shrink) {  // rare once a few units are seen
+    float drop, num_drop;
+    if (ref.move(mx, ex, drop, num_drop)) {  // rare once a few units are seen
       l *= drop;
 #pragma unroll
       for (int d = 0; d < NB; ++d)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[d][e] *= drop * vdrop;
+        for (int e = 0; e < 4; ++e) o[d][e] *= num_drop;
     }
-    const int we = weight_exp(vtop, vref);
-    const float mu = ref.used(), wf = ldexpf(1.f, we);
-    float w[8], sum = 0.f;
+    const float mu = ref.ref, to = W_EXP - ref.num;
+    float w[8];
+    if constexpr (EXACT) {
+      float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float v = s[i / 4][i % 4];
-      if constexpr (BIAS) w[i] = __builtin_amdgcn_exp2f((v - mu) * LOG2E);
-      else w[i] = __builtin_amdgcn_exp2f(fmaf(v, f, (EXACT ? 0.f : (float)we) - mu));
-      sum += w[i];
-      if constexpr (EXACT) w[i] *= wf;
+      for (int i = 0; i < 8; ++i) {
+        const float v = s[i / 4][i % 4];
+        if constexpr (BIAS) w[i] = __builtin_amdgcn_exp2f((v - mu) * LOG2E);
+        else w[i] = __builtin_amdgcn_exp2f(fmaf(v, f, -mu));
+        sum += w[i];
+        w[i] = ldexpf(w[i], ve[EVEN ? i / 4 : i] + (int)to);
+      }
+      l += sum;
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        // (under 2^-60 a half adds nothing in f16; the bound keeps the sum's own scale finite)
+        const float e = fmaxf((float)ve[h] + to, -60.f);
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          w[4 * h + i] = __builtin_amdgcn_exp2f(fmaf(s[h][i], f, e - mu));
+          sum += w[4 * h + i];
+        }
+        l += ldexpf(sum, -(int)e);
+      }
     }
-    l += EXACT ? sum : ldexpf(sum, -we);
     f16x8_t pf[NP];
     f16_planes<NP>(w, pf);
-    Ratio vr[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {  // keys 2 k and 2 k + 1 of the lane's eight
-      const int src = 16 * (k / 2) + 4 * g + 2 * (k % 2);
-      if (EVEN) vr[k] = ratio_of(vs[k / 2 % NE] * vinv, vs[k / 2 % NE] * vinv);
-      else vr[k] = ratio_of(__shfl(vs[0], src, SSD_WAVE) * vinv, __shfl(vs[0], src + 1, SSD_WAVE) * vinv);
-    }
 #pragma unroll
     for (int i = 0; i < VW; ++i) {
       f16x8_t vf[4];
-      columns4(vc[i], vr, vf);
+      columns4(vc[i], vf);
 #pragma unroll
       for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -276,7 +292,7 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
     __builtin_amdgcn_sched_barrier(0);
   }
   if (bad_page) atomicOr(a.status, SSD_DEV_BAD_PAGE);
-  const float back = vref * (1.f / W_TOP);
+  const float back = ldexpf(1.f, (int)ref.num - W_EXP);
   l = col_sum(l);
   // O^T block d, row 4 g + e: dimension NB (4 g + e) + d, so a lane holds DH / 4 consecutive ones
 #pragma unroll
@@ -295,13 +311,12 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
   float M = xm[0][pn];
 #pragma unroll
   for (int w = 1; w < AW; ++w) M = fmaxf(M, xm[w][pn]);
-  const float Mu = M == -INFINITY ? 0.f : M;
   float L = 0.f, f[PART];
 #pragma unroll
   for (int i = 0; i < PART; ++i) f[i] = 0.f;
 #pragma unroll
   for (int w = 0; w < AW; ++w) {
-    const float c = __builtin_amdgcn_exp2f((xm[w][pn] - Mu) * (BIAS ? LOG2E : 1.f));
+    const float c = __builtin_amdgcn_exp2f((xm[w][pn] - M) * (BIAS ? LOG2E : 1.f));
     L += c * xl[w][pn];
 #pragma unroll
     for (int i = 0; i < PART; ++i) f[i] += c * xo[w][pn][d0 + i];
@@ -340,9 +355,9 @@ __global__ __launch_bounds__(MERGE) void cache_attn_merge_kernel(const CacheAttn
   const float* p = a.part + ((size_t)r * a.n_q_heads + h) * splits * (DH + 2);
   if (tid < 64) {  // CACHE_SPLITS_MAX is a wave's lanes
     const float* ml = p + (size_t)splits * DH + 2 * tid;
-    const float mv = tid < splits ? ml[0] : -INFINITY, lv = tid < splits ? ml[1] : 0.f;
+    const float mv = tid < splits ? ml[0] : -FLT_MAX, lv = tid < splits ? ml[1] : 0.f;
     const float M = wave_max(mv);
-    const float w = __builtin_amdgcn_exp2f((mv - (M == -INFINITY ? 0.f : M)) * (a.bias ? LOG2E : 1.f));
+    const float w = __builtin_amdgcn_exp2f((mv - M) * (a.bias ? LOG2E : 1.f));
     c[tid] = w;
     xl[tid] = w * lv;
   }

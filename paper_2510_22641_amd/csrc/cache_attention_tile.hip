@@ -8,12 +8,32 @@ namespace {
 
 constexpr int TKEYS = 64;  // keys a block takes at once
 
+// The largest of either half over the wave's lanes.
+typedef short s16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ s16x2_t wave_max2(s16x2_t v) {
+#pragma unroll
+  for (int i = 1; i < 64; i <<= 1)
+    v = __builtin_elementwise_max(v, __builtin_bit_cast(s16x2_t, __shfl_xor(__builtin_bit_cast(int, v), i, SSD_WAVE)));
+  return v;
+}
+
+// A value that is the same in every lane, known to be.
+__device__ __forceinline__ uint64_t uniform(uint64_t v) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 |
+         (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+}
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // TW * NT * 16 (row, head) pairs of one sequence and cache head a block, NT tiles of 16 a wave.  The
 // block turns 64 keys at a time into f16 operands in LDS, in the order in which the matrix
 // instruction's lanes take them (each a contiguous kilobyte), so a code is converted once for all
 // pairs; a wave's scores stay in its registers and are the operand of the second product, as in
 // the kernel of few rows.  While a unit is worked on, the next one's codes are on their way to
 // registers and the page entries of the one after it to LDS; two buffers, one barrier a unit.
+// Value scales enter the operands as their ratios to the largest of the unit, which then serves all
+// its weights.  That takes bits only where scales lie far apart: such a unit, rare in a sequence's
+// own cache, is gone through once for each group of keys whose scales are near each other, the
+// others masked (scales in registers beside the scores would spill).
 // Bound: vector instructions of the softmax (about nine slots a score, four of them the
 // exponential) beside the matrix instructions (two a 16 x 16 x 32 piece for bf16 rows, four for
 // float32).  4096 bf16 rows of 32 heads of 128 behind 4096 positions: 412 GFLOP in 457 us, 0.90
@@ -32,7 +52,9 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
   __shared__ __attribute__((aligned(16))) float ksc[3][TKEYS], vsc[3][TKEYS];
   __shared__ __attribute__((aligned(16))) uint64_t rows[2][TKEYS];  // bytes from the pools' begin on, of the unit to load next
   __shared__ uint64_t live[3];           // keys of the unit that have a row
-  __shared__ float ktops[3], vtops[3];   // largest scales of the unit
+  __shared__ float ktops[3];             // largest key scale of the unit
+  __shared__ int vtops[3], vexp[3][TKEYS];  // exponents of the largest value scale, or, of the groups
+  __shared__ int vfar[3];                   // of keys where some lie far from it, each key's
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g = lane >> 4;
   const int hk = blockIdx.x % a.n_heads, bt = blockIdx.x / a.n_heads;
@@ -128,7 +150,7 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
         t[2 * h + 1] = ratio_of(c.z, c.w);
       }
       f16x8_t f[4];
-      columns4(vc, t, f);
+      columns4(vc, f, t);
 #pragma unroll
       for (int d = 0; d < 4; ++d) vf[buf][vhalf][4 * vpart + d][lane] = __builtin_bit_cast(uint4, f[d]);
     }
@@ -144,14 +166,21 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
     }
   };
   auto store_scales = [&](int sc, uint32_t row) {
-    const float kt = pow2_of(wave_max(ks1)), vt = pow2_of(wave_max(vs1));
+    const float kt = pow2_of(wave_max(ks1));
     ksc[sc][lane] = ks1 * pow2_inv(kt);
-    vsc[sc][lane] = vs1 * pow2_inv(vt);
+    // of the scales that are not 0, the largest exponent and the smallest one's negative
+    const int ve = exp_of(vs1);
+    const s16x2_t m = wave_max2(s16x2_t{(short)ve, (short)(ve == NO_EXP ? NO_EXP : -ve)});
+    const bool far = m[0] != NO_EXP && m[0] + m[1] > NEAR;
+    const int vt = far ? (ve + NEAR - 1) & -NEAR : m[0];
+    vsc[sc][lane] = ldexpf(1.f, ve - vt);
+    vexp[sc][lane] = vt;
     const uint64_t in = __ballot(row != NO_ROW);
     if (lane == 0) {
       live[sc] = in;
       ktops[sc] = kt;
       vtops[sc] = vt;
+      vfar[sc] = far;
     }
   };
   auto store_row = [&](int buf, uint32_t row) {  // keys without a row read the pools' first: they are masked
@@ -182,12 +211,10 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
     __syncthreads();
   }
 
-  float vref = 0.f;  // largest value scale so far
   for (int x = x0, i0 = 0, i1 = 1, i2 = 2; x < x1; ++x) {
     const int buf = (x - x0) & 1;
     int page3 = -1;
-    const uint64_t in = live[i0];
-    const float ktop = ktops[i0], vtop = vtops[i0];
+    const float ktop = ktops[i0];
     if (x + 1 < x1) {
       request(buf ^ 1);
       if (wave == 0) {
@@ -195,7 +222,19 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
         page3 = entry(x + 3);
       }
     }
-    if (!idle && x * TKEYS <= wlast) {
+    uint64_t rest = !idle && x * TKEYS <= wlast ? uniform(live[i0]) : 0;
+    while (rest) {
+      // (one turn, but for rare units: what each turn loads and computes stays in it)
+      int key0 = x * TKEYS;
+      asm volatile("" : "+s"(key0) : : "memory");
+      uint64_t in = rest;  // the keys of this turn
+      int vtop = uniform(vtops[i0]);
+      if (uniform(vfar[i0])) {
+        const int e = vexp[i0][lane];
+        vtop = __builtin_amdgcn_readlane(e, __builtin_ctzll(rest));
+        in &= __ballot(e == vtop);
+      }
+      rest &= ~in;
       // (operands are read from LDS a group ahead of their products; the scheduler would read each
       // where it is used and wait)
       f32x4_t s[NT][TKEYS / 16];
@@ -220,16 +259,7 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
               s[t][k] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fr[k & 1][st], q[t][st][p], s[t][k], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
-      const bool full = in == ~0ull && x * TKEYS + TKEYS - 1 <= first;  // no key of the unit is masked
-      float vdrop = 1.f;
-      bool vmove = false;
-      if (vtop > vref) {
-        vdrop = vref * pow2_inv(vtop);
-        vref = vtop;
-        vmove = true;
-      }
-      const int we = weight_exp(vtop, vref);
-      const float wf = ldexpf(1.f, we);
+      const bool full = in == ~0ull && key0 + TKEYS - 1 <= first;  // no key of the unit is masked
       f16x8_t pf[NT][TKEYS / 32][NP];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
@@ -239,10 +269,10 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
 #pragma unroll
           for (int i = 0; i < TKEYS / 4; ++i)
             s[t][i / 4][i % 4] = fmaf(s[t][i / 4][i % 4], f,
-                                      bp[max(0, min(pos[t] - (x * TKEYS + 16 * (i / 4) + 4 * g + i % 4), a.n_bias - 1))]);
+                                      bp[max(0, min(pos[t] - (key0 + 16 * (i / 4) + 4 * g + i % 4), a.n_bias - 1))]);
         }
         if (!full) {  // (uniform)
-          const int after = pos[t] - x * TKEYS - 4 * g;  // last of the lane's keys, counted from its first
+          const int after = pos[t] - key0 - 4 * g;  // last of the lane's keys, counted from its first
 #pragma unroll
           for (int i = 0; i < TKEYS / 4; ++i) {
             const int key = 16 * (i / 4) + i % 4;
@@ -254,19 +284,20 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
         for (int i = 1; i < TKEYS / 4; i += 2)  // (the last one twice)
           mx = max3(mx, s[t][i / 4][i % 4], s[t][(i + 1 < TKEYS / 4 ? i + 1 : i) / 4][(i + 1 < TKEYS / 4 ? i + 1 : i) % 4]);
         mx = col_max(mx) * (BIAS ? 1.f : f);
-        float drop;
-        if (ref[t].move(mx, drop) || vmove) {  // rare once a few units are seen
+        float drop, num_drop;
+        if (ref[t].move(mx, (float)vtop, drop, num_drop)) {  // rare once a few units are seen
           l[t] *= drop;
 #pragma unroll
           for (int d = 0; d < NB; ++d)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[t][d][e] *= drop * vdrop;
+            for (int e = 0; e < 4; ++e) o[t][d][e] *= num_drop;
         }
         if (t == NT - 1) {  // the second product's first operands
 #pragma unroll
           for (int d = 0; d < 4; ++d) fr[0][d] = __builtin_bit_cast(f16x8_t, (&vf[buf][0][0][0])[d * 64 + lane]);
         }
-        const float mu = ref[t].used();
+        // (under 2^-60 the keys add nothing in f16; the bound keeps the sum's own scale finite)
+        const float mu = ref[t].ref, we = (float)(vtop + W_EXP) - ref[t].num, se = fmaxf(we, -60.f);
         float sum = 0.f;
 #pragma unroll
         for (int k = 0; k < TKEYS / 32; ++k) {
@@ -275,13 +306,13 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
           for (int i = 0; i < 8; ++i) {
             const float v = s[t][2 * k + i / 4][i % 4];
             if constexpr (BIAS) w[i] = __builtin_amdgcn_exp2f((v - mu) * LOG2E);
-            else w[i] = __builtin_amdgcn_exp2f(fmaf(v, f, (EXACT ? 0.f : (float)we) - mu));
+            else w[i] = __builtin_amdgcn_exp2f(fmaf(v, f, (EXACT ? 0.f : se) - mu));
             sum += w[i];
-            if constexpr (EXACT) w[i] *= wf;
+            if constexpr (EXACT) w[i] = ldexpf(w[i], (int)we);
           }
           f16_planes<NP>(w, pf[t][k]);
         }
-        l[t] += EXACT ? sum : ldexpf(sum, -we);
+        l[t] += EXACT ? sum : ldexpf(sum, -(int)se);
       }
       constexpr int GROUPS = TKEYS / 32 * NB / 4;  // of four operands
 #pragma unroll
@@ -320,11 +351,10 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
     i2 = i;
   }
   if (bad_page) atomicOr(a.status, SSD_DEV_BAD_PAGE);
-  const float back = vref * (1.f / W_TOP);
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int u = uw + 16 * t + n;
-    const float L = col_sum(l[t]);
+    const float L = col_sum(l[t]), back = ldexpf(1.f, (int)ref[t].num - W_EXP);
     if (u >= pairs) continue;
     // O^T block d, row 4 g + e: dimension NB (4 g + e) + d, so a lane holds DH / 4 consecutive ones
     const int j = u / G;
