@@ -11,8 +11,8 @@
 // row's own that follows the largest such product (struct Reference): a key counts there by what it
 // adds to the output, so a block of large values with no weight, or one that the row may not attend,
 // takes no bits from the others.  They are one plane for bf16 rows (2^-11, an eighth of the
-// output's own rounding) and two for float32, between 2^W_EXP and 2^(W_EXP + REF_STEP) for the
-// largest; those under f16's normal numbers are off by 2^-25, 2^-32 of the largest.
+// output's own rounding) and two for float32, up to 2^(W_EXP + REF_STEP) and for the largest seen
+// at least 2^(W_EXP - NEAR - 1); those under f16's normal numbers are off by 2^-25.
 #pragma once
 
 #include "device.h"

@@ -292,15 +292,17 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
     __builtin_amdgcn_sched_barrier(0);
   }
   if (bad_page) atomicOr(a.status, SSD_DEV_BAD_PAGE);
-  const float back = ldexpf(1.f, (int)ref.num - W_EXP);
+  // (divided first: a sum of values may be past the largest number where their mean is not)
   l = col_sum(l);
+  const float inv_l = l == 0.f ? 0.f : 1.f / l, back = ldexpf(1.f, (int)ref.num - W_EXP);  // (NaN stays)
   // O^T block d, row 4 g + e: dimension NB (4 g + e) + d, so a lane holds DH / 4 consecutive ones
 #pragma unroll
   for (int e = 0; e < 4; ++e)
 #pragma unroll
     for (int d = 0; d < NB; d += 4)
       *reinterpret_cast<float4*>(&xo[wave][n][NB * (4 * g + e) + d]) =
-          make_float4(o[d][e] * back, o[d + 1][e] * back, o[d + 2][e] * back, o[d + 3][e] * back);
+          make_float4(o[d][e] * inv_l * back, o[d + 1][e] * inv_l * back, o[d + 2][e] * inv_l * back,
+                      o[d + 3][e] * inv_l * back);
   if (g == 0) { xm[wave][n] = ref.ref; xl[wave][n] = l; }
   __syncthreads();
   // thread (pair, part): the waves' results
@@ -311,15 +313,19 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
   float M = xm[0][pn];
 #pragma unroll
   for (int w = 1; w < AW; ++w) M = fmaxf(M, xm[w][pn]);
-  float L = 0.f, f[PART];
+  float L = 0.f, c[AW], f[PART];
+#pragma unroll
+  for (int w = 0; w < AW; ++w) {
+    c[w] = __builtin_amdgcn_exp2f((xm[w][pn] - M) * (BIAS ? LOG2E : 1.f)) * xl[w][pn];
+    L += c[w];
+  }
+  const float inv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
   for (int i = 0; i < PART; ++i) f[i] = 0.f;
 #pragma unroll
   for (int w = 0; w < AW; ++w) {
-    const float c = __builtin_amdgcn_exp2f((xm[w][pn] - M) * (BIAS ? LOG2E : 1.f));
-    L += c * xl[w][pn];
 #pragma unroll
-    for (int i = 0; i < PART; ++i) f[i] += c * xo[w][pn][d0 + i];
+    for (int i = 0; i < PART; ++i) f[i] += c[w] * inv * xo[w][pn][d0 + i];
   }
   const int pj = pu / G, ph = hk * G + (pu - pj * G);
   const size_t row = (size_t)(r0 + pj);
@@ -332,21 +338,18 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
     }
     return;
   }
-  const float inv = L == 0.f ? 0.f : 1.f / L;  // (NaN stays)
-#pragma unroll
-  for (int i = 0; i < PART; ++i) f[i] *= inv;
   store_result<T, DH, PART>(a, row, ph, d0, f);
 }
 
 // The splits' results of row blockIdx.y of sequence blockIdx.z and one head: per pair `splits` rows
-// of DH sums, then their (maximum, sum) pairs.  Thread groups of DH / 4 lanes take every eighth (or
+// of DH means, then their (reference, sum of weights) pairs.  Thread groups of DH / 4 lanes take every eighth (or
 // sixteenth) split, four dimensions a lane, and meet in LDS: the order of the sums is fixed.
 constexpr int MERGE = 256;
 template <typename T, int DH>
 __global__ __launch_bounds__(MERGE) void cache_attn_merge_kernel(const CacheAttnArgs a, const int splits) {
   constexpr int LANES = DH / 4, GROUPS = MERGE / LANES;
   __shared__ float xo[GROUPS][DH];
-  __shared__ float c[CACHE_SPLITS_MAX], xl[CACHE_SPLITS_MAX];
+  __shared__ float c[CACHE_SPLITS_MAX];  // shares of the splits
   const int h = blockIdx.x, tid = threadIdx.x;
   int r0, nr;
   seq_rows(a, blockIdx.z, r0, nr);
@@ -357,9 +360,8 @@ __global__ __launch_bounds__(MERGE) void cache_attn_merge_kernel(const CacheAttn
     const float* ml = p + (size_t)splits * DH + 2 * tid;
     const float mv = tid < splits ? ml[0] : -FLT_MAX, lv = tid < splits ? ml[1] : 0.f;
     const float M = wave_max(mv);
-    const float w = __builtin_amdgcn_exp2f((mv - M) * (a.bias ? LOG2E : 1.f));
-    c[tid] = w;
-    xl[tid] = w * lv;
+    const float w = __builtin_amdgcn_exp2f((mv - M) * (a.bias ? LOG2E : 1.f)) * lv, L = wave_sum(w);
+    c[tid] = L == 0.f ? 0.f : w / L;
   }
   __syncthreads();
   const int grp = tid / LANES, d = (tid % LANES) * 4;
@@ -373,15 +375,13 @@ __global__ __launch_bounds__(MERGE) void cache_attn_merge_kernel(const CacheAttn
   *reinterpret_cast<float4*>(&xo[grp][d]) = f;
   __syncthreads();
   if (tid < DH) {
-    float L = 0.f, v = 0.f;
-    for (int s = 0; s < splits; ++s) L += xl[s];
+    float v = 0.f;
 #pragma unroll
     for (int k = 0; k < GROUPS; ++k) v += xo[k][tid];
-    const float inv = L == 0.f ? 0.f : 1.f / L;
     if (sizeof(T) == 4 && a.out_planes)
-      store_planes1(a.out_planes + plane_at(r, h * DH + tid, (a.rows + 15) >> 4), v * inv);
+      store_planes1(a.out_planes + plane_at(r, h * DH + tid, (a.rows + 15) >> 4), v);
     else
-      store_elem(reinterpret_cast<T*>(a.out) + (size_t)r * a.ldo + (size_t)h * DH + tid, v * inv);
+      store_elem(reinterpret_cast<T*>(a.out) + (size_t)r * a.ldo + (size_t)h * DH + tid, v);
   }
 }
 

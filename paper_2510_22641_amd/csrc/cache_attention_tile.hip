@@ -359,12 +359,12 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
     // O^T block d, row 4 g + e: dimension NB (4 g + e) + d, so a lane holds DH / 4 consecutive ones
     const int j = u / G;
     const size_t row = (size_t)(r0 + j), head = (size_t)(hk * G + (u - j * G));
-    const float inv = splits > 1 ? back : L == 0.f ? 0.f : back / L;  // (NaN stays)
+    const float inv = L == 0.f ? 0.f : 1.f / L;  // (NaN stays; before `back`: the mean may be a number where the sum is none)
     float f[DH / 4];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
-      for (int d = 0; d < NB; ++d) f[NB * e + d] = o[t][d][e] * inv;
+      for (int d = 0; d < NB; ++d) f[NB * e + d] = o[t][d][e] * inv * back;
     if (splits > 1) {
       float* p = a.part + (row * a.n_q_heads + head) * splits * (DH + 2);
       store_out<float, DH / 4>(p + (size_t)split * DH + g * (DH / 4), f, false);

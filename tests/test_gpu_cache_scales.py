@@ -147,3 +147,18 @@ def test_later_rows_values_leave_earlier_rows_alone(rows, page, dtype):
         c.v_scale[0, p] = 2.0 ** min(-20 + 9 * i, 110)
     q = torch.randn(rows, 4, 64, generator=g).to(dtype).cuda()
     check(c, q, [rows], 0.125)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=IDS)
+@pytest.mark.parametrize("lens,rows,heads,group,d_head", [(700, 1, 32, 1, 64), (5000, 1, 1, 4, 128), (600, 9, 2, 1, 64),
+                                                          (900, 20, 2, 3, 64), (3000, 17, 1, 2, 128), (40, 200, 2, 1, 64)])
+def test_means_of_values_near_the_largest_number(lens, rows, heads, group, d_head, dtype):
+    """Equal weights over hundreds of values of up to 2^127: their sum is no float32 number, their mean
+    is, whole and in ranges of keys."""
+    c, g = make_cache([lens], heads, d_head, 16, max_seq=lens + rows + 1)
+    c.grow([rows])
+    c.v_scale.fill_(2.0 ** 121)
+    c.v_codes.copy_(c.v_codes.abs().clamp(max=63))
+    q = torch.zeros(rows, heads * group, d_head, dtype=dtype, device="cuda")
+    check(c, q, [rows], 1.0)
+    check(c, q, [rows], 1.0, torch.randn(heads * group, 200, generator=g).cuda())
