@@ -5,7 +5,7 @@
 // and the products run on the f16 matrix instruction.  Queries enter scaled by a power of two that puts
 // their row's largest element into [2^14, 2^15): bf16 ones as one f16 plane (11 bits against
 // their 8), float32 ones as two (22 bits: an element is off by at most 2^-23 of itself, less than a
-// sum of 64 products in float32 loses).
+// sum of 64 products in float32 loses), either to 2^-39 of the row's largest.
 //
 // Weights enter the second product times their key's value scale, under a power of two of the
 // row's own that follows the largest such product (struct Reference): a key counts there by what it
@@ -101,11 +101,18 @@ __device__ __forceinline__ int exp_of(float s) {
 }
 __device__ __forceinline__ float pow2_inv(float p) { return __uint_as_float(0x7f000000u - __float_as_uint(p)); }
 
-// The factor of a row's products over keys of largest key scale ktop.
-__device__ __forceinline__ float score_factor(float qf, float ktop) {
-  const float f = qf * ktop;
-  return f < FLT_MIN ? FLT_MIN : f;
-}
+// What turns a product of a row of exponent qe and keys of scale 2^ke into a score, positive: |scale|,
+// `unit` times, its mantissa and exponent apart, so that no part alone has to be in range.  (Products
+// stay under 2^30: a score whose factor is no normal number is nothing.)
+struct Factor {
+  float m;
+  int e;
+  __device__ __forceinline__ Factor(float scale, float unit) {
+    m = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(frexpf(fabsf(scale), &e) * unit)));
+    e = __builtin_amdgcn_readfirstlane(e);
+  }
+  __device__ __forceinline__ float of(int qe, int ke) const { return fmaxf(ldexpf(m, e + qe + ke), FLT_MIN); }
+};
 
 // Eight floats as N f16 planes, each the rounding of what the one before leaves.
 template <int N>
@@ -142,10 +149,10 @@ __device__ __forceinline__ float col_sum(float v) {
 }
 
 // The matrix operand of a query row: lane (row l % 16, g = l / 16) takes elements 64 (t / 2) + 16 g +
-// 8 (t % 2) + i at step t, with the sign of `scale`.  Returns what turns a product with it into a
-// score: |scale| 2^(e - 14), positive, or NaN where an element is not finite.
+// 8 (t % 2) + i at step t, with the sign of `scale`, times 2^-(the exponent returned); NaN throughout
+// where an element or `scale` is not finite.
 template <typename T, int DH>
-__device__ __forceinline__ float load_query(const T* row, int g, float scale, f16x8_t (&q)[DH / 32][Planes<T>::N]) {
+__device__ __forceinline__ int load_query(const T* row, int g, float scale, f16x8_t (&q)[DH / 32][Planes<T>::N]) {
   float f[DH / 32][8], top = 0.f;
   bool bad = false;
 #pragma unroll
@@ -158,16 +165,16 @@ __device__ __forceinline__ float load_query(const T* row, int g, float scale, f1
       bad |= !(fabsf(v) <= FLT_MAX);
     }
   top = col_max(bad ? INFINITY : top);
-  const bool fine = top <= FLT_MAX, some = top > 0.f && fine && scale != 0.f;
+  const bool fine = top <= FLT_MAX && fabsf(scale) <= FLT_MAX, some = top > 0.f && fine && scale != 0.f;
   const int e = some ? ilogbf(top) : 0;
 #pragma unroll
   for (int t = 0; t < DH / 32; ++t) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[t][i] = some ? ldexpf(scale < 0.f ? -f[t][i] : f[t][i], 14 - e) : 0.f;
+    for (int i = 0; i < 8; ++i)
+      f[t][i] = some ? ldexpf(scale < 0.f ? -f[t][i] : f[t][i], 14 - e) : fine ? 0.f : NAN;
     f16_planes<Planes<T>::N>(f[t], q[t]);
   }
-  const float to = ldexpf(fabsf(scale), e - 14);
-  return !fine ? NAN : !some ? 1.f : to < FLT_MIN ? FLT_MIN : to;
+  return some ? e - 14 : 0;
 }
 
 // The rows of sequence b: first row and count, kept inside the buffers whatever row_start holds.

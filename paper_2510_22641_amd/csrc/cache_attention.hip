@@ -145,8 +145,9 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
   if (x0 + wave < x1) ahead = entries(x0 + wave);
   const int ul = min(u0 + n, pairs - 1), jl = ul / G, hq = hk * G + (ul - jl * G), pos = base + jl;  // this lane's pair
   f16x8_t q[KS][NP];
-  const float qf = load_query<T, DH>(reinterpret_cast<const T*>(a.q) + (size_t)(r0 + jl) * a.ldq + (size_t)hq * DH, g,
-                                     a.scale, q) * (BIAS ? 1.f : LOG2E);
+  const Factor factor(a.scale, BIAS ? 1.f : LOG2E);
+  const int qe = load_query<T, DH>(reinterpret_cast<const T*>(a.q) + (size_t)(r0 + jl) * a.ldq + (size_t)hq * DH, g,
+                                   a.scale, q);
   const float* bias_row = BIAS ? a.bias + (size_t)hq * a.n_bias : nullptr;
   Reference<BIAS> ref;
   float l = 0.f;  // sum of the weights
@@ -208,7 +209,7 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
         for (int p = NP - 1; p >= 0; --p) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[st][p], s[h], 0, 0, 0);
       }
     }
-    const float f = score_factor(qf, ktop);
+    const float f = factor.of(qe, exp_of(ktop));
     if constexpr (BIAS) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[i / 4][i % 4] = fmaf(s[i / 4][i % 4], f, bias[i]);

@@ -52,7 +52,7 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
   __shared__ __attribute__((aligned(16))) float ksc[3][TKEYS], vsc[3][TKEYS];
   __shared__ __attribute__((aligned(16))) uint64_t rows[2][TKEYS];  // bytes from the pools' begin on, of the unit to load next
   __shared__ uint64_t live[3];           // keys of the unit that have a row
-  __shared__ float ktops[3];             // largest key scale of the unit
+  __shared__ int ktops[3];                  // exponent of the unit's largest key scale
   __shared__ int vtops[3], vexp[3][TKEYS];  // exponents of the largest value scale, or, of the groups
   __shared__ int vfar[3];                   // of keys where some lie far from it, each key's
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -79,9 +79,10 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
   const int uw = u0 + 16 * NT * wave;
   const bool idle = uw >= pairs;
   const int first = base + min(uw, pairs - 1) / G, wlast = base + min(uw + 16 * NT - 1, pairs - 1) / G;
-  int pos[NT], hq[NT];
+  const Factor factor(a.scale, BIAS ? 1.f : LOG2E);
+  int pos[NT], hq[NT], qe[NT];
   f16x8_t q[NT][KS][NP];
-  float qf[NT], l[NT];
+  float l[NT];
   Reference<BIAS> ref[NT];
   f32x4_t o[NT][NB];
 #pragma unroll
@@ -90,7 +91,7 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
     hq[t] = hk * G + (u - j * G);
     pos[t] = base + j;
     const T* qp = reinterpret_cast<const T*>(a.q) + (size_t)(r0 + j) * a.ldq + (size_t)hq[t] * DH;
-    qf[t] = load_query<T, DH>(qp, g, a.scale, q[t]) * (BIAS ? 1.f : LOG2E);
+    qe[t] = load_query<T, DH>(qp, g, a.scale, q[t]);
     l[t] = 0.f;
 #pragma unroll
     for (int d = 0; d < NB; ++d) o[t][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -178,7 +179,7 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
     const uint64_t in = __ballot(row != NO_ROW);
     if (lane == 0) {
       live[sc] = in;
-      ktops[sc] = kt;
+      ktops[sc] = exp_of(kt);
       vtops[sc] = vt;
       vfar[sc] = far;
     }
@@ -214,7 +215,7 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
   for (int x = x0, i0 = 0, i1 = 1, i2 = 2; x < x1; ++x) {
     const int buf = (x - x0) & 1;
     int page3 = -1;
-    const float ktop = ktops[i0];
+    const int ktop = uniform(ktops[i0]);
     if (x + 1 < x1) {
       request(buf ^ 1);
       if (wave == 0) {
@@ -263,7 +264,7 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
       f16x8_t pf[NT][TKEYS / 32][NP];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const float f = score_factor(qf[t], ktop);
+        const float f = factor.of(qe[t], ktop);
         if constexpr (BIAS) {
           const float* bp = a.bias + (size_t)hq[t] * a.n_bias;
 #pragma unroll

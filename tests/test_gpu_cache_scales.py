@@ -162,3 +162,20 @@ def test_means_of_values_near_the_largest_number(lens, rows, heads, group, d_hea
     q = torch.zeros(rows, heads * group, d_head, dtype=dtype, device="cuda")
     check(c, q, [rows], 1.0)
     check(c, q, [rows], 1.0, torch.randn(heads * group, 200, generator=g).cuda())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=IDS)
+@pytest.mark.parametrize("rows,page", [(1, 16), (1, 3), (9, 16), (40, 16), (140, 5)])
+@pytest.mark.parametrize("query,keys,scale", [(-115, 115, 1.0), (-124, 121, 1.0), (-90, 110, 2.0 ** -30),
+                                              (100, -98, 2.0 ** -9), (-30, -60, 2.0 ** 85), (60, 60, 2.0 ** -127)])
+def test_queries_and_keys_of_extreme_magnitudes(query, keys, scale, rows, page, dtype):
+    """Tiny queries over huge keys and the like: the factor between their products and the scores is
+    formed from exponents, and neither part of it has to be a normal number."""
+    c, g = make_cache([130], 2, 64, page, max_seq=400)
+    c.grow([rows])
+    c.v_scale.fill_(0.125)
+    c.k_scale.fill_(2.0 ** keys)
+    q = torch.randn(rows, 4, 64, generator=g).double() * 2.0 ** (query - 7)
+    q = (torch.where(q.abs() < 2.0 ** -126, 0.0, q)).to(dtype).cuda()
+    check(c, q, [rows], scale)
+    check(c, q, [rows], -scale, torch.randn(4, 90, generator=g).cuda())
