@@ -114,6 +114,12 @@ struct Factor {
   __device__ __forceinline__ float of(int qe, int ke) const { return fmaxf(ldexpf(m, e + qe + ke), FLT_MIN); }
 };
 
+// A product that is rounded whatever becomes of it.
+__device__ __forceinline__ float rounded(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
+
 // Eight floats as N f16 planes, each the rounding of what the one before leaves.
 template <int N>
 __device__ __forceinline__ void f16_planes(const float (&f)[8], f16x8_t (&out)[N]) {

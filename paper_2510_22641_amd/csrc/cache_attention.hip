@@ -51,7 +51,6 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
   constexpr int NB = DH / 16;  // output blocks of 16 dimensions
   constexpr int VW = DH / 64;  // dwords of V a lane and key
   constexpr int NP = Planes<T>::N;
-  constexpr bool EXACT = BIAS || sizeof(T) == 4 || !EVEN;  // weights from the scores' differences alone
   __shared__ float xo[AW][16][DH + 4];
   __shared__ float xm[AW][16], xl[AW][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -210,10 +209,10 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
       }
     }
     const float f = factor.of(qe, exp_of(ktop));
-    if constexpr (BIAS) {
+    // (scores are rounded before anything is subtracted: a product and its reference that went through
+    // other roundings would differ by far more than REF_STEP where scores are large)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[i / 4][i % 4] = fmaf(s[i / 4][i % 4], f, bias[i]);
-    }
+    for (int i = 0; i < 8; ++i) s[i / 4][i % 4] = BIAS ? fmaf(s[i / 4][i % 4], f, bias[i]) : rounded(s[i / 4][i % 4], f);
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (BIAS) request_bias(x + AW);
     request_k(next);
@@ -226,19 +225,18 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
         if (row == NO_ROW || x * UNIT + src > pos) s[i / 4][i % 4] = -INFINITY;
       }
     }
-    const float c = BIAS ? 1.f : f;
     auto half_max = [&](int h) { return max3(max3(s[h][0], s[h][1], s[h][2]), s[h][3], s[h][3]); };
-    const float mx = col_max(max3(half_max(0), half_max(1), half_max(1))) * c;
+    const float mx = col_max(max3(half_max(0), half_max(1), half_max(1)));
     float ex;
     if constexpr (EVEN) {
       ex = (float)max(ve[0], ve[1]);
       if (abs(ve[0] - ve[1]) > NEAR)  // (uniform)
-        ex = fmaxf(fmaf(col_max(half_max(0)) * c - mx, ref.UNIT, (float)ve[0]),
-                   fmaf(col_max(half_max(1)) * c - mx, ref.UNIT, (float)ve[1]));
+        ex = fmaxf(fmaf(col_max(half_max(0)) - mx, ref.UNIT, (float)ve[0]),
+                   fmaf(col_max(half_max(1)) - mx, ref.UNIT, (float)ve[1]));
     } else {
       ex = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) ex = fmaxf(ex, fmaf(s[i / 4][i % 4] * c - mx, ref.UNIT, (float)ve[i]));
+      for (int i = 0; i < 8; ++i) ex = fmaxf(ex, fmaf(s[i / 4][i % 4] - mx, ref.UNIT, (float)ve[i]));
       ex = col_max(ex);
     }
     float drop, num_drop;
@@ -249,32 +247,13 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[d][e] *= num_drop;
     }
-    const float mu = ref.ref, to = W_EXP - ref.num;
+    const int to = W_EXP - (int)ref.num;
     float w[8];
-    if constexpr (EXACT) {
-      float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float v = s[i / 4][i % 4];
-        if constexpr (BIAS) w[i] = __builtin_amdgcn_exp2f((v - mu) * LOG2E);
-        else w[i] = __builtin_amdgcn_exp2f(fmaf(v, f, -mu));
-        sum += w[i];
-        w[i] = ldexpf(w[i], ve[EVEN ? i / 4 : i] + (int)to);
-      }
-      l += sum;
-    } else {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        // (under 2^-60 a half adds nothing in f16; the bound keeps the sum's own scale finite)
-        const float e = fmaxf((float)ve[h] + to, -60.f);
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          w[4 * h + i] = __builtin_amdgcn_exp2f(fmaf(s[h][i], f, e - mu));
-          sum += w[4 * h + i];
-        }
-        l += ldexpf(sum, -(int)e);
-      }
+    for (int i = 0; i < 8; ++i) {
+      w[i] = __builtin_amdgcn_exp2f((s[i / 4][i % 4] - ref.ref) * ref.UNIT);
+      l += w[i];
+      w[i] = ldexpf(w[i], ve[EVEN ? i / 4 : i] + to);
     }
     f16x8_t pf[NP];
     f16_planes<NP>(w, pf);

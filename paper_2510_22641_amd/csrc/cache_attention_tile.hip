@@ -264,7 +264,7 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
       f16x8_t pf[NT][TKEYS / 32][NP];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        const float f = factor.of(qe[t], ktop);
+        float f = factor.of(qe[t], ktop);
         if constexpr (BIAS) {
           const float* bp = a.bias + (size_t)hq[t] * a.n_bias;
 #pragma unroll
@@ -298,7 +298,20 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
           for (int d = 0; d < 4; ++d) fr[0][d] = __builtin_bit_cast(f16x8_t, (&vf[buf][0][0][0])[d * 64 + lane]);
         }
         // (under 2^-60 the keys add nothing in f16; the bound keeps the sum's own scale finite)
-        const float mu = ref[t].ref, we = (float)(vtop + W_EXP) - ref[t].num, se = fmaxf(we, -60.f);
+        const float we = (float)(vtop + W_EXP) - ref[t].num, se = fmaxf(we, -60.f);
+        float from = (EXACT ? 0.f : se) - ref[t].ref;
+        // A fused product less the reference, which is a rounded one: large scores are rounded first (one
+        // step of 2^16 is 2^-7).
+        const bool large = !BIAS && fabsf(ref[t].ref) > 65536.f;
+        if (__any(large)) {  // (such rows alone)
+#pragma unroll
+          for (int i = 0; i < TKEYS / 4; ++i) {
+            const float v = s[t][i / 4][i % 4];
+            s[t][i / 4][i % 4] = large ? rounded(v, f) - ref[t].ref : v;
+          }
+          f = large ? 1.f : f;
+          from = large ? EXACT ? 0.f : se : from;
+        }
         float sum = 0.f;
 #pragma unroll
         for (int k = 0; k < TKEYS / 32; ++k) {
@@ -306,8 +319,8 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const float v = s[t][2 * k + i / 4][i % 4];
-            if constexpr (BIAS) w[i] = __builtin_amdgcn_exp2f((v - mu) * LOG2E);
-            else w[i] = __builtin_amdgcn_exp2f(fmaf(v, f, (EXACT ? 0.f : se) - mu));
+            if constexpr (BIAS) w[i] = __builtin_amdgcn_exp2f((v - ref[t].ref) * LOG2E);
+            else w[i] = __builtin_amdgcn_exp2f(fmaf(v, f, from));
             sum += w[i];
             if constexpr (EXACT) w[i] = ldexpf(w[i], (int)we);
           }

@@ -179,3 +179,49 @@ def test_queries_and_keys_of_extreme_magnitudes(query, keys, scale, rows, page, 
     q = (torch.where(q.abs() < 2.0 ** -126, 0.0, q)).to(dtype).cuda()
     check(c, q, [rows], scale)
     check(c, q, [rows], -scale, torch.randn(4, 90, generator=g).cuda())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=IDS)
+@pytest.mark.parametrize("rows,page", SHAPES + [(260, 16)])
+@pytest.mark.parametrize("scale", [2.0 ** 17 * 0.7, -2.0 ** 24 * 0.9, 2.0 ** 40 * 0.7, -2.0 ** 100 * 0.6])
+def test_scores_of_any_magnitude(rows, page, scale, dtype):
+    """Two keys share every row's largest score, far over the others': the output is the mean of their
+    values, however coarse the scores' own type is there."""
+    c, g = make_cache([290], 2, 64, page, max_seq=600)
+    c.grow([rows])
+    c.v_scale.fill_(2.0 ** -6)
+    c.k_scale.fill_(1.0)
+    c.k_codes.clamp_(min=-100, max=100)
+    q = torch.randint(1, 4, (rows, 4, 64), generator=g).to(dtype).cuda()  # products are exact
+    want = 0.0
+    for p in (3, 260):
+        page_id, o = int(c.page_table[0, p // page]), p % page
+        c.k_codes[0, page_id, :, o] = 101 if scale > 0 else -101  # 64 and more over the others
+        want = want + c.v_codes[0, page_id, :, o].double().cpu() * 2.0 ** -7
+    rs = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    got = c.attend(0, q, rs, rows, scale).double().cpu()
+    want = want.repeat_interleave(2, 0)[None].expand_as(got)
+    # equal weights: planes of 2^-22 (bf16: 2^-11) of values of at most 127 2^-6 each, a division, a rounding
+    lim = 2.0 ** (-22 if dtype == F32 else -11) * 2 + want.abs() * (2.0 ** -22 if dtype == F32 else 2.0 ** -8)
+    assert bool(((got - want).abs() <= lim).all()) and int(c.status) == 0
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=IDS)
+@pytest.mark.parametrize("rows,page", SHAPES + [(260, 16)])
+@pytest.mark.parametrize("magnitude", [2.0 ** 22, 2.0 ** 31, 2.0 ** 90])
+def test_scores_far_below_zero_give_means_of_the_values(rows, page, magnitude, dtype):
+    """A score's step is past any difference that a weight resolves: still each row is some mean."""
+    c, g = make_cache([290], 2, 64, page, max_seq=600)
+    c.grow([rows])
+    c.v_scale.fill_(2.0 ** -6)
+    c.k_scale.fill_(magnitude)
+    c.k_codes.copy_(-torch.randint(1, 100, c.k_codes.shape, generator=g).to(torch.int8))
+    q = (torch.rand(rows, 4, 64, generator=g) + 0.5).to(dtype).cuda()
+    rs = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    got = c.attend(0, q, rs, rows, 0.125).float()
+    at = torch.arange(c.lens[0], device="cuda")
+    v = c.v_codes[0, c.page_table[0, at // page].long(), :, at % page].float() * 2.0 ** -6  # [n, heads, d_head]
+    hi, lo = (t.repeat_interleave(2, 0) for t in (v.amax(0), v.amin(0)))
+    slack = 2.0 ** -7 * float(v.abs().max())
+    assert bool(((got <= hi + slack) & (got >= lo - slack)).all()) and int(c.status) == 0
+    assert bool((got.abs().amax(-1) > 0).all())
