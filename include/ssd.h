@@ -359,7 +359,7 @@ int ssd_sync_status(ssd_ctx* ctx, int32_t* status);
  * Keys and values of one layer as int8 codes in pages, with one float32 scale for each page and
  * head (a block): value = code * scale.  Scales are powers of two of 2^-100 and more, as
  * ssd_cache_store writes them (or 0 where it has not written yet): the attention works with their
- * ratios in 16 bits.  These calls need no context; a context whose kvdtype is
+ * exponents alone.  These calls need no context; a context whose kvdtype is
  * SSD_I8 makes them itself.  They are asynchronous on `stream` (a hipStream_t; NULL: the null
  * stream of the current device) and may be captured into a graph; the pointers belong to the
  * stream's device, whichever device is current.  d_status is one device word of the caller's, into

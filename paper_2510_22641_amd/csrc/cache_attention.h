@@ -1,8 +1,7 @@
 // Device helpers shared by the kernels of attention over the 8-bit paged cache.
 //
-// Codes are whole numbers below 2^7 and scales powers of two, so a code times the ratio of its key's
-// scale to the largest one of the keys it is worked on with is exact in f16 down to ratios of 2^-24,
-// and the products run on the f16 matrix instruction.  Queries enter scaled by a power of two that puts
+// Codes are whole numbers below 2^7 and scales powers of two: a code, or a code times a ratio of scales
+// down to 2^-24, is exact in f16, so the products run on the f16 matrix instruction.  Queries enter scaled by a power of two that puts
 // their row's largest element into [2^14, 2^15): bf16 ones as one f16 plane (11 bits against
 // their 8), float32 ones as two (22 bits: an element is off by at most 2^-23 of itself, less than a
 // sum of 64 products in float32 loses), either to 2^-39 of the row's largest.
@@ -66,12 +65,13 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t w_flipped, uint32_t sel) 
   return __builtin_bit_cast(uint32_t, v - f16x2_t{(_Float16)1152.f, (_Float16)1152.f});
 }
 
-// Eight consecutive codes of a key's row.
-__device__ __forceinline__ f16x8_t codes8(uint32_t a, uint32_t b, const Ratio& t) {
+// Eight consecutive codes of a key's row, by code_pair's last argument.
+template <typename... R>
+__device__ __forceinline__ f16x8_t codes8(uint32_t a, uint32_t b, const R&... t) {
   a ^= 0x80808080u;
   b ^= 0x80808080u;
-  return f16_frag(code_pair(a, 0x04010400, t), code_pair(a, 0x04030402, t), code_pair(b, 0x04010400, t),
-                  code_pair(b, 0x04030402, t));
+  return f16_frag(code_pair(a, 0x04010400, t...), code_pair(a, 0x04030402, t...), code_pair(b, 0x04010400, t...),
+                  code_pair(b, 0x04030402, t...));
 }
 
 // Eight keys' dwords, four dimensions each: operand d is dimension d of the eight keys, by code_pair's
@@ -92,14 +92,16 @@ __device__ __forceinline__ void columns4(const uint32_t (&w)[8], f16x8_t (&out)[
   for (int d = 0; d < 4; ++d) out[d] = f16_frag(p[d][0], p[d][1], p[d][2], p[d][3]);
 }
 
-// A scale's power of two (0 where no block has been written), its exponent and its reciprocal (a
-// large number for 0, whose blocks' ratios are 0 all the same).
-__device__ __forceinline__ float pow2_of(float s) { return __uint_as_float(__float_as_uint(s) & 0x7f800000u); }
+// A scale's exponent.
 __device__ __forceinline__ int exp_of(float s) {
   const int e = (int)(__float_as_uint(s) >> 23 & 0xff);
   return e ? e - 127 : NO_EXP;
 }
-__device__ __forceinline__ float pow2_inv(float p) { return __uint_as_float(0x7f000000u - __float_as_uint(p)); }
+
+// Two exponents in one word.
+__device__ __forceinline__ int pair_of(int k, int v) { return v << 16 | (k & 0xffff); }
+__device__ __forceinline__ int first_of(int p) { return (int16_t)p; }
+__device__ __forceinline__ int second_of(int p) { return p >> 16; }
 
 // What turns a product of a row of exponent qe and keys of scale 2^ke into a score, positive: |scale|,
 // `unit` times, its mantissa and exponent apart, so that no part alone has to be in range.  (Products
@@ -235,8 +237,8 @@ __device__ __forceinline__ void store_result(const CacheAttnArgs& a, size_t row,
 // (Row (page n_heads + head) page_size + offset of the pools; there are fewer than 2^32 of them.)
 constexpr uint32_t NO_ROW = 0xffffffffu;
 
-// Value scales of keys that one exponent serves differ by at most this many powers of two.
-constexpr int NEAR = 4;
+// Value (key) scales of keys that one exponent serves differ by at most this many powers of two.
+constexpr int NEAR = 4, K_NEAR = 16;
 
 // The running references of a row's softmax.  Scores are t = s * f (+ bias); without a bias f carries
 // log2 e and t is in powers of two, with one t stays in natural units, where the type's lowest value

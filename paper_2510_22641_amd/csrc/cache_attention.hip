@@ -37,9 +37,9 @@ __device__ __forceinline__ V scalar_load(const V* p) {
 // their use; its scales one unit ahead and its page-table entries two (codes of a second or third
 // unit on their way in registers of their own measured 2 and 3% slower).  EVEN:
 // pages hold a multiple of 16 positions, so a half lies in one page and its entry and scales are
-// scalars; else every key has its own, which cross lanes.  The codes of V are operands as they are;
-// their scales multiply the weights.  Each wave keeps its own references and sums; they meet in LDS
-// once.
+// scalars; else every key has its own, which cross lanes.  The codes are operands as they are; their
+// scales multiply the scores and the weights.  Each wave keeps its own references and sums; they
+// meet in LDS once.
 // Bound: for long contexts the bytes of the codes, which lie scattered in pieces of a page and head
 // (one token, 32 heads of 128 over 32768 positions: 269 MB in 52 us and 5 for the merge; 32 tokens of
 // 2048 positions, 8 cache heads: 134 MB in 33 us; of 1 to 4096: 130 MB in 41); for short ones the
@@ -176,43 +176,44 @@ __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_at
     ahead = then;
     const bool rows = EVEN ? cur.row[0] != NO_ROW && cur.row[NE - 1] != NO_ROW : __all(cur.row[0] != NO_ROW);
     const bool full = rows && x * UNIT + UNIT - 1 <= first;  // no key of it is masked
-    // key scales over the unit's largest, exponents of the value scales: of the halves, or the lane's keys
-    float ks[NE];
-    int ve[EVEN ? 2 : 8];
+    // exponents of the scales: of the halves, or the lane's keys
+    int ke[EVEN ? 2 : 8], ve[EVEN ? 2 : 8];
 #pragma unroll
     for (int h = 0; h < NE; ++h) {
-      ks[h] = cur.row[h] != NO_ROW ? cur.ks[h] : 0.f;
+      ke[h] = cur.row[h] != NO_ROW ? exp_of(cur.ks[h]) : NO_EXP;
       ve[h] = cur.row[h] != NO_ROW ? exp_of(cur.vs[h]) : NO_EXP;
     }
-    float ktop = fmaxf(ks[0], ks[NE - 1]);
     if constexpr (!EVEN) {
+      const int own = pair_of(ke[0], ve[0]);
 #pragma unroll
-      for (int i = 1; i < 32; i <<= 1) ktop = fmaxf(ktop, __shfl_xor(ktop, i, SSD_WAVE));
-      const int own = ve[0];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) ve[i] = __shfl(own, 16 * (i / 4) + 4 * g + i % 4, SSD_WAVE);
+      for (int i = 0; i < 8; ++i) {
+        const int p = __shfl(own, 16 * (i / 4) + 4 * g + i % 4, SSD_WAVE);
+        ke[i] = first_of(p);
+        ve[i] = second_of(p);
+      }
     }
-    ktop = pow2_of(ktop);
-    const float kinv = pow2_inv(ktop);
     f32x4_t s[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const float k = (EVEN ? ks[h % NE] : __shfl(ks[0], 16 * h + n, SSD_WAVE)) * kinv;
-      const Ratio kr = ratio_of(k, k);
       s[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
       const uint32_t* kw = reinterpret_cast<const uint32_t*>(&kc[h][0]);
 #pragma unroll
       for (int st = 0; st < KS; ++st) {
-        const f16x8_t kf = codes8(kw[2 * st], kw[2 * st + 1], kr);
+        const f16x8_t kf = codes8(kw[2 * st], kw[2 * st + 1]);
 #pragma unroll
         for (int p = NP - 1; p >= 0; --p) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, q[st][p], s[h], 0, 0, 0);
       }
     }
-    const float f = factor.of(qe, exp_of(ktop));
     // (scores are rounded before anything is subtracted: a product and its reference that went through
     // other roundings would differ by far more than REF_STEP where scores are large)
+    float f[EVEN ? 2 : 8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s[i / 4][i % 4] = BIAS ? fmaf(s[i / 4][i % 4], f, bias[i]) : rounded(s[i / 4][i % 4], f);
+    for (int i = 0; i < (EVEN ? 2 : 8); ++i) f[i] = factor.of(qe, ke[i]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float v = s[i / 4][i % 4], c = f[EVEN ? i / 4 : i];
+      s[i / 4][i % 4] = BIAS ? fmaf(v, c, bias[i]) : rounded(v, c);
+    }
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (BIAS) request_bias(x + AW);
     request_k(next);

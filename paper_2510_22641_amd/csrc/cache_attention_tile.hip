@@ -30,10 +30,10 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 // pairs; a wave's scores stay in its registers and are the operand of the second product, as in
 // the kernel of few rows.  While a unit is worked on, the next one's codes are on their way to
 // registers and the page entries of the one after it to LDS; two buffers, one barrier a unit.
-// Value scales enter the operands as their ratios to the largest of the unit, which then serves all
-// its weights.  That takes bits only where scales lie far apart: such a unit, rare in a sequence's
-// own cache, is gone through once for each group of keys whose scales are near each other, the
-// others masked (scales in registers beside the scores would spill).
+// Scales enter the operands as their ratios to the largest of the unit, which then serves all its
+// scores or weights.  That takes bits only where scales lie far apart: such a unit, rare in a
+// sequence's own cache, is gone through once for each group of keys whose scales are near each
+// other, the others masked (scales in registers beside the scores would spill).
 // Bound: vector instructions of the softmax (about nine slots a score, four of them the
 // exponential) beside the matrix instructions (two a 16 x 16 x 32 piece for bf16 rows, four for
 // float32).  4096 bf16 rows of 32 heads of 128 behind 4096 positions: 412 GFLOP in 457 us, 0.90
@@ -52,9 +52,8 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
   __shared__ __attribute__((aligned(16))) float ksc[3][TKEYS], vsc[3][TKEYS];
   __shared__ __attribute__((aligned(16))) uint64_t rows[2][TKEYS];  // bytes from the pools' begin on, of the unit to load next
   __shared__ uint64_t live[3];           // keys of the unit that have a row
-  __shared__ int ktops[3];                  // exponent of the unit's largest key scale
-  __shared__ int vtops[3], vexp[3][TKEYS];  // exponents of the largest value scale, or, of the groups
-  __shared__ int vfar[3];                   // of keys where some lie far from it, each key's
+  __shared__ int tops[3], group[3][TKEYS];  // exponents of the largest key and value scale, each key's group's
+  __shared__ int apart[3];                  // whether the unit has several groups
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g = lane >> 4;
   const int hk = blockIdx.x % a.n_heads, bt = blockIdx.x / a.n_heads;
@@ -167,21 +166,20 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
     }
   };
   auto store_scales = [&](int sc, uint32_t row) {
-    const float kt = pow2_of(wave_max(ks1));
-    ksc[sc][lane] = ks1 * pow2_inv(kt);
-    // of the scales that are not 0, the largest exponent and the smallest one's negative
-    const int ve = exp_of(vs1);
-    const s16x2_t m = wave_max2(s16x2_t{(short)ve, (short)(ve == NO_EXP ? NO_EXP : -ve)});
-    const bool far = m[0] != NO_EXP && m[0] + m[1] > NEAR;
-    const int vt = far ? (ve + NEAR - 1) & -NEAR : m[0];
+    // of the scales that are not 0, the largest exponents and the smallest ones' negatives
+    const int ke = exp_of(ks1), ve = exp_of(vs1);
+    const s16x2_t k = wave_max2(s16x2_t{(short)ke, (short)(ke == NO_EXP ? NO_EXP : -ke)}),
+                  v = wave_max2(s16x2_t{(short)ve, (short)(ve == NO_EXP ? NO_EXP : -ve)});
+    const bool far = k[0] + k[1] > K_NEAR || v[0] + v[1] > NEAR;
+    const int kt = far ? (ke + K_NEAR - 1) & -K_NEAR : k[0], vt = far ? (ve + NEAR - 1) & -NEAR : v[0];
+    ksc[sc][lane] = ldexpf(1.f, ke - kt);
     vsc[sc][lane] = ldexpf(1.f, ve - vt);
-    vexp[sc][lane] = vt;
+    group[sc][lane] = pair_of(kt, vt);
     const uint64_t in = __ballot(row != NO_ROW);
     if (lane == 0) {
       live[sc] = in;
-      ktops[sc] = exp_of(kt);
-      vtops[sc] = vt;
-      vfar[sc] = far;
+      tops[sc] = pair_of(kt, vt);
+      apart[sc] = far;
     }
   };
   auto store_row = [&](int buf, uint32_t row) {  // keys without a row read the pools' first: they are masked
@@ -215,7 +213,6 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
   for (int x = x0, i0 = 0, i1 = 1, i2 = 2; x < x1; ++x) {
     const int buf = (x - x0) & 1;
     int page3 = -1;
-    const int ktop = uniform(ktops[i0]);
     if (x + 1 < x1) {
       request(buf ^ 1);
       if (wave == 0) {
@@ -229,12 +226,13 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
       int key0 = x * TKEYS;
       asm volatile("" : "+s"(key0) : : "memory");
       uint64_t in = rest;  // the keys of this turn
-      int vtop = uniform(vtops[i0]);
-      if (uniform(vfar[i0])) {
-        const int e = vexp[i0][lane];
-        vtop = __builtin_amdgcn_readlane(e, __builtin_ctzll(rest));
-        in &= __ballot(e == vtop);
+      int top = uniform(tops[i0]);
+      if (uniform(apart[i0])) {
+        const int own = group[i0][lane];
+        top = __builtin_amdgcn_readlane(own, __builtin_ctzll(rest));
+        in &= __ballot(own == top);
       }
+      const int ktop = first_of(top), vtop = second_of(top);
       rest &= ~in;
       // (operands are read from LDS a group ahead of their products; the scheduler would read each
       // where it is used and wait)

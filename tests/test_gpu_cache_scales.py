@@ -225,3 +225,41 @@ def test_scores_far_below_zero_give_means_of_the_values(rows, page, magnitude, d
     slack = 2.0 ** -7 * float(v.abs().max())
     assert bool(((got <= hi + slack) & (got >= lo - slack)).all()) and int(c.status) == 0
     assert bool((got.abs().amax(-1) > 0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=IDS)
+@pytest.mark.parametrize("rows,page", SHAPES)
+def test_keys_of_large_scale_and_no_weight(rows, page, dtype):
+    """Keys of a scale 2^30 and more over the others', against the queries: their scores are far below,
+    and the others' as exact as without them."""
+    c, g = make_cache([300], 2, 64, page, max_seq=600)
+    c.grow([rows])
+    c.v_scale.fill_(2.0 ** -6)
+    c.k_scale.fill_(2.0 ** -6)
+    q = (torch.randn(rows, 4, 64, generator=g) / 4 + 1).to(dtype).cuda()
+    for at, e in ((8, 24), (100, 30), (102, 90), (250, 28)):
+        p = pages_of(c, 0, at, at + 1)
+        c.k_scale[0, p] = 2.0 ** e
+        c.k_codes[0, p] = -c.k_codes[0, p].abs() - 1
+        c.k_codes[0, p] = c.k_codes[0, p].clamp(min=-127)
+    check(c, q, [rows], 0.125)
+    check(c, q, [rows], 0.125, torch.randn(4, 90, generator=g).cuda())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=IDS)
+@pytest.mark.parametrize("rows,page", [(2, 1), (9, 2), (20, 5), (40, 16), (140, 5), (260, 16)])
+def test_later_rows_keys_leave_earlier_rows_alone(rows, page, dtype):
+    """A row's scores do not depend on the key scales of the rows behind it."""
+    c, g = make_cache([45], 4, 64, page, max_seq=600)
+    c.grow([rows])
+    pages = c.page_table[0, :-(-c.lens[0] // page)].tolist()
+    q = torch.randn(rows, 4, 64, generator=g).to(dtype).cuda()
+    for first in (1, rows // 2):  # the rows from `first` on are masked for those before it
+        c.k_scale.fill_(2.0 ** -6)
+        for p in pages[(45 + first) // page + 1:]:
+            c.k_scale[0, p] = 2.0 ** 40
+        n = min((45 + first) // page * page + page - 45, rows)  # rows before those pages
+        rs = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+        got = c.attend(0, q, rs, rows, 0.125).double().cpu()[:n]
+        ref, tol = reference(c, q[:n], [45], [n], 0.125)
+        assert bool(((got - ref).abs() <= tol).all())
