@@ -438,8 +438,11 @@ typedef struct {
   int32_t* status;
 } ssd_cache_attn;
 
-/* Bytes of workspace (256-byte aligned) a call with these sizes needs, 0 for none; the pointers are
- * not looked at.  A call writes it before it reads it, so calls on one stream may share it. */
+/* Bytes of workspace (256-byte aligned) that a call with these sizes asks for, 0 for none and for sizes
+ * that the call refuses; neither pointers nor strides are looked at.  They grow with rows, n_q_heads,
+ * d_head and max_len and depend on nothing else: the workspace of the largest call serves the smaller
+ * ones, at most 2^16 (d_head + 2) floats.  A call writes it before it reads it, so calls on one
+ * stream may share it. */
 size_t ssd_cache_attention_workspace(const ssd_cache* cache, const ssd_cache_attn* attn);
 int ssd_cache_attention(const ssd_cache* cache, const ssd_cache_attn* attn, void* d_workspace,
                         size_t workspace_bytes, void* stream);

@@ -432,22 +432,20 @@ int cache_attn_splits(const CacheAttnArgs& a) {
   if (want > most) want = most;
   if (want > CACHE_SPLITS_MAX) want = CACHE_SPLITS_MAX;
   if (block_pairs(a) == 16 && (a.max_len <= 512 || (want < 4 && a.max_len < 2048))) want = 1;
+  // Blocks of n pairs hold rows * n_q_heads <= blocks n pairs, and a split call has blocks * splits <
+  // 256 + blocks <= 512 of them (n <= 128), or with n = 64 < 512 + blocks <= 1024: CACHE_PARTS_MAX
+  // splits of a pair, but for rows that belong to no sequence.
+  const long long room = CACHE_PARTS_MAX / ((long long)a.rows * a.n_q_heads);
+  if (want > room) want = room;
   return want < 1 ? 1 : (int)want;
 }
 
-size_t cache_attn_part_floats(const CacheAttnArgs& a) {
-  const int splits = cache_attn_splits(a);
-  return splits > 1 ? (size_t)a.rows * a.n_q_heads * splits * (a.d_head + 2) : 0;
-}
-
-// Blocks of n pairs hold rows * n_q_heads <= blocks n pairs, and a split call has blocks * splits <
-// 256 + blocks <= 512 of them (n <= 128), or with n = 64 < 512 + blocks <= 1024: 2^16 splits of a pair.
-size_t cache_attn_part_bound(size_t rows, int n_q_heads, int d_head, int max_len) {
+size_t cache_attn_part_floats(size_t rows, int n_q_heads, int d_head, int max_len) {
   size_t splits = ((size_t)max_len + 127) / 128;
   if (splits > CACHE_SPLITS_MAX) splits = CACHE_SPLITS_MAX;
   if (splits < 2) return 0;
   const size_t n = rows * n_q_heads * splits;
-  return (n < 1 << 16 ? n : 1 << 16) * (d_head + 2);
+  return (n < CACHE_PARTS_MAX ? n : CACHE_PARTS_MAX) * (d_head + 2);
 }
 
 hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t s) {

@@ -370,6 +370,7 @@ hipError_t launch_bias_table(const float* rel_bias, const int32_t* bucket, int H
 constexpr int PAGE_MAP_MAX_BATCH = 4096;  // two prefix sums over the sequences in LDS
 constexpr int CACHE_MAX_PAGE = 256;       // positions per page
 constexpr int CACHE_SPLITS_MAX = 64;
+constexpr int CACHE_PARTS_MAX = 1 << 16;  // (row, head, key range) triples of a call in ranges
 // The factor of page_of (device.h).
 inline uint32_t page_inv(int page_size) { return (uint32_t)(((1ull << 32) + page_size - 1) / page_size); }
 
@@ -437,9 +438,8 @@ struct CacheAttnArgs {
   float* part;        // cache_attn_part_floats of them
 };
 int cache_attn_splits(const CacheAttnArgs& a);
-size_t cache_attn_part_floats(const CacheAttnArgs& a);
-// At least those of every call of up to `rows` rows with max_len.
-size_t cache_attn_part_bound(size_t rows, int n_q_heads, int d_head, int max_len);
+// Room for the partial results of every call of up to `rows` rows with up to max_len positions.
+size_t cache_attn_part_floats(size_t rows, int n_q_heads, int d_head, int max_len);
 hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t s);
 // Many rows: blocks of n (row, head) pairs (64, 128 or 256), without the merge of the splits.
 hipError_t launch_cache_attn_tile(const CacheAttnArgs& a, int n, int splits, hipStream_t s);

@@ -135,7 +135,7 @@ bool make_layout(const ssd_dims& d, Layout& L, bool allow_fold = true, bool allo
     // 8-bit caches: a pass's keys and values in float32, their slots, the attention's partials
     L.kv_rows = take(i8 ? 2 * R * HD * 4 : 0);
     L.kv_slot = take(i8 ? R * 8 : 0);
-    L.cache_part = take(i8 ? cache_attn_part_bound(rows, d.n_heads, d.d_head, d.max_seq) * 4 : 0);
+    L.cache_part = take(i8 ? cache_attn_part_floats(rows, d.n_heads, d.d_head, d.max_seq) * 4 : 0);
   }
   L.vis = take(d.arch == SSD_ARCH_T5 ? B * (size_t)d.n_visual * D * 4 : 0);
   {
@@ -993,7 +993,7 @@ int cache_rows(const ssd_cache* cache, int rows, const int64_t* d_slot, const vo
   return SSD_OK;
 }
 
-// The sizes of an attention call, checked.
+// The sizes of an attention call that its workspace depends on, checked.
 int cache_attn_sizes(const ssd_cache* cache, const ssd_cache_attn* t, CacheAttnArgs& a) {
   if (!cache || !t) return SSD_ERR_ARG;
   if (!cache_shape_ok(cache) || !cache_pages_ok(cache->page_size, t->max_pages)) return SSD_ERR_SHAPE;
@@ -1002,11 +1002,8 @@ int cache_attn_sizes(const ssd_cache* cache, const ssd_cache_attn* t, CacheAttnA
       t->max_rows > 1 << 24 || t->max_len < 1 || t->n_q_heads < 1 || t->n_q_heads > 4096 ||
       t->n_q_heads % cache->n_heads)
     return SSD_ERR_SHAPE;
-  if (!t->row_start && t->rows != (int64_t)t->B * t->max_rows) return SSD_ERR_SHAPE;
   const int64_t tiles = ((int64_t)t->max_rows * (t->n_q_heads / cache->n_heads) + 15) / 16;
   if ((int64_t)t->B * tiles * cache->n_heads > INT32_MAX) return SSD_ERR_SHAPE;
-  const int64_t hd = (int64_t)t->n_q_heads * cache->d_head;
-  if (t->ldq < hd || t->ldo < hd) return SSD_ERR_ARG;
   cache_fields(cache, a);
   a.B = t->B; a.rows = t->rows; a.max_rows = t->max_rows; a.max_len = t->max_len;
   a.n_q_heads = t->n_q_heads; a.dtype = t->dtype; a.max_pages = t->max_pages;
@@ -1626,7 +1623,7 @@ int ssd_cache_load(const ssd_cache* cache, int rows, const int64_t* d_slot, void
 size_t ssd_cache_attention_workspace(const ssd_cache* cache, const ssd_cache_attn* attn) {
   CacheAttnArgs a;
   if (cache_attn_sizes(cache, attn, a)) return 0;
-  return cache_attn_part_floats(a) * sizeof(float);
+  return cache_attn_part_floats(a.rows, a.n_q_heads, a.d_head, a.max_len) * sizeof(float);
 }
 
 int ssd_cache_attention(const ssd_cache* cache, const ssd_cache_attn* attn, void* d_workspace,
@@ -1634,12 +1631,15 @@ int ssd_cache_attention(const ssd_cache* cache, const ssd_cache_attn* attn, void
   CacheAttnArgs a;
   int rc = cache_attn_sizes(cache, attn, a);
   if (rc) return rc;
+  if (!attn->row_start && a.rows != (int64_t)a.B * a.max_rows) return SSD_ERR_SHAPE;
+  const int64_t hd = (int64_t)a.n_q_heads * a.d_head;
+  if (attn->ldq < hd || attn->ldo < hd) return SSD_ERR_ARG;
   if (!cache_pointers_ok(cache) || !attn->seq_len || !attn->page_table || !attn->status) return SSD_ERR_ARG;
   if (a.rows == 0) return SSD_OK;
   const size_t elem = a.dtype == SSD_BF16 ? 2 : 4;
   if (!attn->q || !attn->out || (uintptr_t)attn->q % elem || (uintptr_t)attn->out % elem) return SSD_ERR_ARG;
   if (attn->bias ? attn->n_bias < 1 : attn->n_bias != 0) return SSD_ERR_ARG;
-  const size_t bytes = cache_attn_part_floats(a) * sizeof(float);
+  const size_t bytes = cache_attn_part_floats(a.rows, a.n_q_heads, a.d_head, a.max_len) * sizeof(float);
   if (bytes && (!d_workspace || (uintptr_t)d_workspace % 256)) return SSD_ERR_ARG;
   if (workspace_bytes < bytes) return SSD_ERR_CAPACITY;
   a.q = attn->q; a.ldq = attn->ldq; a.out = attn->out; a.ldo = attn->ldo;
