@@ -382,9 +382,10 @@ typedef struct {
  * they are, and *d_taken receives the pages taken.  d_free NULL (n_free 0): the table has the pages
  * already and is only read.  d_row_start [B + 1] receives the first row of each sequence, its new
  * positions being consecutive rows, and their total; d_slot [max_rows] the slot page * page_size +
- * offset of each row, -1 for rows behind the last.  1 <= B <= 4096.  A negative count, a length
- * outside the table, rows past max_rows (cut) or pages past n_free (table entries -1) set
- * SSD_DEV_CAPACITY, a page outside [0, n_pages) SSD_DEV_BAD_PAGE; the rows concerned get slot -1. */
+ * offset of each row, -1 for rows behind the last.  1 <= B <= 4096; max_rows and n_free at most 2^30.
+ * A negative count, a length outside the table, rows past max_rows (cut) or pages past n_free (table
+ * entries -1) set SSD_DEV_CAPACITY, a page outside [0, n_pages) SSD_DEV_BAD_PAGE; the rows concerned
+ * get slot -1. */
 int ssd_page_map(int B, int page_size, int n_pages, int max_pages, const int32_t* d_seq_len,
                  const int32_t* d_new, const int32_t* d_free, int n_free, int32_t* d_page_table,
                  int32_t* d_row_start, int64_t* d_slot, int max_rows, int32_t* d_taken,
@@ -400,7 +401,9 @@ int ssd_page_map(int B, int page_size, int n_pages, int max_pages, const int32_t
  * becomes the smallest power of two s (at least 2^-100) such that 127 s covers its rows' largest
  * magnitude, those in front rescaled; codes are the nearest whole numbers (ties to even).  8 bits
  * hold neither infinities nor NaN: SSD_DEV_NOT_FINITE is set, an infinity becomes the block's
- * largest value, a NaN zero.  A slot outside the pools sets SSD_DEV_BAD_PAGE and is skipped. */
+ * largest value, a NaN zero.  A slot outside the pools sets SSD_DEV_BAD_PAGE and is skipped.  Up to
+ * 2^24 rows; sizes past what one grid has threads for (about 2^35 elements) are SSD_ERR_SHAPE, in this
+ * call and the next two. */
 int ssd_cache_store(const ssd_cache* cache, int rows, const int64_t* d_slot, const void* d_k,
                     const void* d_v, int64_t ld, int dtype, int32_t* d_status, void* stream);
 

@@ -459,20 +459,32 @@ hipError_t launch_page_map(const PageMapArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Rows a wave: one while that leaves the device room; of long prompts 16, a usual page's worth, since
+// most waves of one row would find that their row begins no run.
+static int store_window(const CacheRowsArgs& a) { return a.rows > 256 ? 16 : 1; }
+static int store_groups(const CacheRowsArgs& a) { return (2 * a.n_heads + STORE_WAVES - 1) / STORE_WAVES; }
+static uint64_t store_blocks(const CacheRowsArgs& a) {
+  const int w = store_window(a);
+  return (uint64_t)((a.rows + w - 1) / w) * store_groups(a);
+}
+static uint64_t load_blocks(const CacheRowsArgs& a) {
+  return ((uint64_t)a.rows * (a.n_heads * a.d_head / 8) + 255) / 256;
+}
+
+bool cache_rows_fit(const CacheRowsArgs& a) {
+  return store_blocks(a) * (64 * STORE_WAVES) <= MAX_GRID_THREADS && load_blocks(a) * 256 <= MAX_GRID_THREADS;
+}
+
 hipError_t launch_cache_store(const CacheRowsArgs& a, hipStream_t s) {
   if (a.rows < 1) return hipSuccess;
-  // One row a wave while that leaves the device room; long prompts 16, a usual page's worth, since
-  // most waves of one row would find that their row begins no run.
-  const int window = a.rows > 256 ? 16 : 1;
-  const int groups = (2 * a.n_heads + STORE_WAVES - 1) / STORE_WAVES;
-  const dim3 grid((unsigned)((a.rows + window - 1) / window) * groups);
+  const int window = store_window(a), groups = store_groups(a);
+  const dim3 grid((unsigned)store_blocks(a));
   return a.dtype == 1 ? store_t<bf16_t>(a, window, groups, grid, s) : store_t<float>(a, window, groups, grid, s);
 }
 
 hipError_t launch_cache_load(const CacheRowsArgs& a, hipStream_t s) {
   if (a.rows < 1) return hipSuccess;
-  const size_t lanes = (size_t)a.rows * (a.n_heads * a.d_head / 8);
-  const dim3 grid((unsigned)((lanes + 255) / 256), 2), block(256);
+  const dim3 grid((unsigned)load_blocks(a), 2), block(256);
   const size_t elem = a.dtype == 1 ? 2 : 4;
   const bool vec = aligned(a.k_out, a.ld, elem, 16) && aligned(a.v_out, a.ld, elem, 16);
   if (a.dtype == 1) {

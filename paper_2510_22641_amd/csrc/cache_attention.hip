@@ -440,6 +440,10 @@ int cache_attn_splits(const CacheAttnArgs& a) {
   return want < 1 ? 1 : (int)want;
 }
 
+bool cache_attn_fits(const CacheAttnArgs& a) {  // (blocks of up to eight waves)
+  return (uint64_t)blocks_of(a) * 512 <= MAX_GRID_THREADS;
+}
+
 size_t cache_attn_part_floats(size_t rows, int n_q_heads, int d_head, int max_len) {
   size_t splits = ((size_t)max_len + 127) / 128;
   if (splits > CACHE_SPLITS_MAX) splits = CACHE_SPLITS_MAX;

@@ -369,6 +369,7 @@ hipError_t launch_bias_table(const float* rel_bias, const int32_t* bucket, int H
 
 constexpr int PAGE_MAP_MAX_BATCH = 4096;  // two prefix sums over the sequences in LDS
 constexpr int CACHE_MAX_PAGE = 256;       // positions per page
+constexpr uint64_t MAX_GRID_THREADS = (1ull << 32) - 1;  // of a grid's first dimension
 constexpr int CACHE_SPLITS_MAX = 64;
 constexpr int CACHE_PARTS_MAX = 1 << 16;  // (row, head, key range) triples of a call in ranges
 // The factor of page_of (device.h).
@@ -409,6 +410,7 @@ struct CacheRowsArgs {
   int dtype;
   int32_t* status;
 };
+bool cache_rows_fit(const CacheRowsArgs& a);  // whether both launches' grids are within the device's
 hipError_t launch_cache_store(const CacheRowsArgs& a, hipStream_t s);
 hipError_t launch_cache_load(const CacheRowsArgs& a, hipStream_t s);
 
@@ -438,6 +440,7 @@ struct CacheAttnArgs {
   float* part;        // cache_attn_part_floats of them
 };
 int cache_attn_splits(const CacheAttnArgs& a);
+bool cache_attn_fits(const CacheAttnArgs& a);  // as cache_rows_fit
 // Room for the partial results of every call of up to `rows` rows with up to max_len positions.
 size_t cache_attn_part_floats(size_t rows, int n_q_heads, int d_head, int max_len);
 hipError_t launch_cache_attention(const CacheAttnArgs& a, hipStream_t s);

@@ -990,6 +990,7 @@ int cache_rows(const ssd_cache* cache, int rows, const int64_t* d_slot, const vo
   if (rows > 0 && (!d_slot || !d_k || !d_v || (uintptr_t)d_k % elem || (uintptr_t)d_v % elem)) return SSD_ERR_ARG;
   cache_fields(cache, a);
   a.rows = rows; a.slot = d_slot; a.ld = ld; a.dtype = dtype; a.status = d_status;
+  if (!cache_rows_fit(a)) return SSD_ERR_SHAPE;
   return SSD_OK;
 }
 
@@ -1002,11 +1003,10 @@ int cache_attn_sizes(const ssd_cache* cache, const ssd_cache_attn* t, CacheAttnA
       t->max_rows > 1 << 24 || t->max_len < 1 || t->n_q_heads < 1 || t->n_q_heads > 4096 ||
       t->n_q_heads % cache->n_heads)
     return SSD_ERR_SHAPE;
-  const int64_t tiles = ((int64_t)t->max_rows * (t->n_q_heads / cache->n_heads) + 15) / 16;
-  if ((int64_t)t->B * tiles * cache->n_heads > INT32_MAX) return SSD_ERR_SHAPE;
   cache_fields(cache, a);
   a.B = t->B; a.rows = t->rows; a.max_rows = t->max_rows; a.max_len = t->max_len;
   a.n_q_heads = t->n_q_heads; a.dtype = t->dtype; a.max_pages = t->max_pages;
+  if (!cache_attn_fits(a)) return SSD_ERR_SHAPE;
   return SSD_OK;
 }
 
@@ -1579,7 +1579,9 @@ int ssd_page_map(int B, int page_size, int n_pages, int max_pages, const int32_t
                  int32_t* d_status, void* stream) {
   if (!d_seq_len || !d_new || !d_page_table || !d_row_start || !d_taken || !d_status) return SSD_ERR_ARG;
   if (n_free < 0 || max_rows < 0 || (n_free > 0 && !d_free) || (max_rows > 0 && !d_slot)) return SSD_ERR_ARG;
-  if (B < 1 || B > PAGE_MAP_MAX_BATCH || n_pages < 1 || !cache_pages_ok(page_size, max_pages)) return SSD_ERR_SHAPE;
+  if (B < 1 || B > PAGE_MAP_MAX_BATCH || n_pages < 1 || !cache_pages_ok(page_size, max_pages) || n_free > 1 << 30 ||
+      max_rows > 1 << 30)  // (their indices and strides stay in 32 bits)
+    return SSD_ERR_SHAPE;
   PageMapArgs a;
   a.B = B; a.page_size = page_size; a.n_pages = n_pages; a.max_pages = max_pages;
   a.seq_len = d_seq_len; a.pos_off = 0; a.new_rows = d_new; a.new_const = 0;
