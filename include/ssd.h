@@ -408,7 +408,8 @@ int ssd_cache_store(const ssd_cache* cache, int rows, const int64_t* d_slot, con
                     const void* d_v, int64_t ld, int dtype, int32_t* d_status, void* stream);
 
 /* The values of rows read back: d_k and d_v laid out as for ssd_cache_store receive code * scale
- * of slot d_slot[r] (-1: the row is left as it is), in any order and as often as wanted. */
+ * of slot d_slot[r] (-1: the row is left as it is), in any order and as often as wanted.  A value past
+ * dtype's largest number, as code 64 of scale 2^122 is, becomes that number. */
 int ssd_cache_load(const ssd_cache* cache, int rows, const int64_t* d_slot, void* d_k, void* d_v,
                    int64_t ld, int dtype, int32_t* d_status, void* stream);
 

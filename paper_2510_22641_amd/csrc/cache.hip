@@ -341,7 +341,8 @@ __global__ __launch_bounds__(64 * STORE_WAVES) void cache_store_kernel(const Cac
       for (int i = 0; i < 4; ++i) held = fmaxf(held, fabsf(code_at(w, i)));
     }
     held *= s_old;
-    if (!(held <= FLT_MAX)) held = 0.f;  // a stored scale that is not finite counts as zero
+    // codes over 63 of scale 2^122 are past the largest number (a stored scale that is none counts as zero)
+    if (!(held <= FLT_MAX)) held = s_old <= FLT_MAX ? FLT_MAX : 0.f;
     // largest magnitude as bits, which order as the numbers do
     uint32_t top = __float_as_uint(held);
 #pragma unroll
@@ -415,6 +416,11 @@ __global__ __launch_bounds__(256) void cache_load_kernel(const CacheRowsArgs a) 
   for (int i = 0; i < 4; ++i) {
     f[i] = code_at(w.x, i) * sc;
     f[4 + i] = code_at(w.y, i) * sc;
+  }
+  if (sc >= 0x1p122f) {  // code 64 stands for the largest numbers, which rounded up to it
+    const float most = sizeof(T) == 4 ? FLT_MAX : 0x1.fep127f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = fminf(fmaxf(f[i], -most), most);
   }
   T* o = reinterpret_cast<T*>(is_v ? a.v_out : a.k_out) + r * a.ld + c;
   if constexpr (!VEC) {
