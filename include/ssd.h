@@ -24,7 +24,7 @@
  *   - With an SSD_I8 cache each pass stores its keys and values as ssd_cache_store does, rows of a
  *     pass on one page at once; the codes in a page that is filled over several passes are rounded
  *     again where its scale rises, so they depend on how its rows came (a draft's first, then the
- *     verify's).  An infinity or NaN among them sets SSD_DEV_NOT_FINITE.
+ *     verify's; a rejected draft of large values leaves the rows in front coarser).  An infinity or NaN among them sets SSD_DEV_NOT_FINITE.
  *   - Matrices are row-major [out][in] (y = W x).  Matrices, embeddings and visual tokens are
  *     in `wdtype`; norm gains, imitation-network biases and the relative-position bias table are
  *     float32.  KV pools are in `kvdtype`.
@@ -399,7 +399,9 @@ int ssd_page_map(int B, int page_size, int n_pages, int max_pages, const int32_t
  * the call, as ssd_page_map lays them, and are stored in that order; a page whose runs have another
  * page's between them ends up with a mixture of them.  The block's scale
  * becomes the smallest power of two s (at least 2^-100) such that 127 s covers its rows' largest
- * magnitude, those in front rescaled; codes are the nearest whole numbers (ties to even).  8 bits
+ * magnitude, those in front rescaled; codes are the nearest whole numbers (ties to even).  So a row is
+ * off by at most s / 2 after its own store, and by less than the largest s that its block has had since
+ * then after more of them (each rise rounds it again, a fall does not).  8 bits
  * hold neither infinities nor NaN: SSD_DEV_NOT_FINITE is set, an infinity becomes the block's
  * largest value, a NaN zero.  A slot outside the pools sets SSD_DEV_BAD_PAGE and is skipped.  Up to
  * 2^24 rows; sizes past what one grid has threads for (about 2^35 elements) are SSD_ERR_SHAPE, in this

@@ -2,8 +2,11 @@
 //
 // A block is one page of one head: page_size rows of d_head int8 codes c with one scale s, a power
 // of two; the row's values are c s.  With the largest magnitude a of the block's rows, s is the
-// smallest 2^e (e >= -100) with a <= 127 2^e: dividing by it is exact, so a value is off by at most
-// half a code, s / 2 <= a / 127, and a block whose scale falls again is rescaled without loss.
+// smallest 2^e (e >= -100) with a <= 127 2^e: dividing by it is exact, so a store rounds a value once, by
+// at most half a code, s / 2 <= a / 127.  A later store on its block that raises the scale rounds it
+// again, by half a code of the new scale: over all of them less than one code of the largest scale
+// that the block has had since the row came, rows given up again among its causes.  A scale that
+// falls rounds nothing, and brings nothing back.
 #include "device.h"
 #include "kernels.h"
 
