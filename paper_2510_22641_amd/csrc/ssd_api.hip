@@ -197,7 +197,7 @@ bool dims_ok(const ssd_dims* d) {
   if (d->max_batch < 1 || d->max_batch > 256) return false;
   if (d->max_gamma < 0 || d->max_gamma > 32) return false;
   // (1024: the longest cache the attention kernels are tested with; their page arithmetic holds to 2^15)
-  // (8-bit caches: the length up to which the rotary and bias tables of a context are tested)
+  // (8-bit caches: the longest contexts whose tables, prompts and last positions are tested)
   if (d->max_seq < 2 || d->max_seq > (i8 ? 65536 : 1024)) return false;
   if (i8 && !cache_pages_ok(d->page_size, d->max_pages)) return false;
   if (d->max_prompt < 1 || d->page_size < 1 || d->max_pages < 1) return false;
