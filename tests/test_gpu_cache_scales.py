@@ -263,3 +263,26 @@ def test_later_rows_keys_leave_earlier_rows_alone(rows, page, dtype):
         got = c.attend(0, q, rs, rows, 0.125).double().cpu()[:n]
         ref, tol = reference(c, q[:n], [45], [n], 0.125)
         assert bool(((got - ref).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=IDS)
+@pytest.mark.parametrize("rows,page", SHAPES)
+def test_blocks_that_were_never_written(rows, page, dtype):
+    """A scale of 0 makes keys and values of zeros, whatever the codes are: among others, and alone."""
+    c, g = make_cache([290], 2, 64, page, max_seq=600)
+    c.grow([rows])
+    c.v_scale.fill_(2.0 ** -6)
+    c.k_scale.fill_(2.0 ** -6)
+    q = torch.randn(rows, 4, 64, generator=g).to(dtype).cuda()
+    for first, last in ((0, 1), (37, 120), (280, 290 + rows)):
+        c.v_scale[0, pages_of(c, 0, first, last)] = 0
+        c.k_scale[0, pages_of(c, 0, first, last)] = 0
+    check(c, q, [rows], 0.125)
+    check(c, q, [rows], 0.125, torch.randn(4, 300, generator=g).cuda())
+    c.v_scale.fill_(0)
+    check(c, q, [rows], 0.125)
+    c.k_scale.fill_(0)
+    rs = torch.tensor([0, rows], dtype=torch.int32, device="cuda")
+    assert not bool(c.attend(0, q, rs, rows, 0.125).any())
+    # a factor that is no number is in every row that has a key
+    assert bool(c.attend(0, q, rs, rows, math.nan).isnan().all())
