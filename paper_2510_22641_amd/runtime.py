@@ -151,8 +151,9 @@ class PagedCache:
                 not 1 <= B <= self.max_batch or row_start.device != self.seq_len.device:
             raise ValueError("row_start: int32 [B + 1] expected")
         if bias is not None and (bias.dtype != torch.float32 or bias.dim() != 2 or not bias.is_contiguous()
-                                 or bias.shape[0] != heads or bias.device != self.seq_len.device):
-            raise ValueError("bias: float32 [query heads, n] expected")
+                                 or bias.shape[0] != heads or bias.shape[1] < 1
+                                 or bias.device != self.seq_len.device):
+            raise ValueError("bias: float32 [query heads, n], n >= 1, expected")
         if out is None:
             out = torch.zeros(q.shape, dtype=q.dtype, device=self.device)
         ldo = self._rows(out, heads, "out")

@@ -47,3 +47,12 @@ def test_attention(abi, B, max_rows, heads, kv_heads):
                             scale=1.0, status=P)
     assert abi.ssd_cache_attention_workspace(cache, at) == 0
     assert _code(abi.ssd_cache_attention, cache, at, P, 1 << 40, None) == abi.SSD_ERR_SHAPE
+
+
+def test_a_bias_without_distances_is_no_bias_to_leave_out():
+    import torch
+    from paper_2510_22641_amd import runtime
+    c = runtime.PagedCache(1, 2, 64, 2, 64, 5, device="cpu")
+    q, rs = torch.zeros(3, 2, 64), torch.tensor([0, 1, 3], dtype=torch.int32)
+    with pytest.raises(ValueError):
+        c.attend(0, q, rs, 2, 1.0, torch.zeros(2, 0))
