@@ -166,10 +166,10 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
     }
   };
   auto store_scales = [&](int sc, uint32_t row) {
-    // of the scales that are not 0, the largest exponents and the smallest ones' negatives
+    // the largest exponents of the unit's keys, and the smallest ones' negatives
     const int ke = exp_of(ks1), ve = exp_of(vs1);
-    const s16x2_t k = wave_max2(s16x2_t{(short)ke, (short)(ke == NO_EXP ? NO_EXP : -ke)}),
-                  v = wave_max2(s16x2_t{(short)ve, (short)(ve == NO_EXP ? NO_EXP : -ve)});
+    const s16x2_t k = wave_max2(s16x2_t{(short)ke, (short)(row == NO_ROW ? NO_EXP : -ke)}),
+                  v = wave_max2(s16x2_t{(short)ve, (short)(row == NO_ROW ? NO_EXP : -ve)});
     const bool far = k[0] + k[1] > K_NEAR || v[0] + v[1] > NEAR;
     const int kt = far ? (ke + K_NEAR - 1) & -K_NEAR : k[0], vt = far ? (ve + NEAR - 1) & -NEAR : v[0];
     ksc[sc][lane] = ldexpf(1.f, ke - kt);

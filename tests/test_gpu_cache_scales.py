@@ -286,3 +286,20 @@ def test_blocks_that_were_never_written(rows, page, dtype):
     assert not bool(c.attend(0, q, rs, rows, 0.125).any())
     # a factor that is no number is in every row that has a key
     assert bool(c.attend(0, q, rs, rows, math.nan).isnan().all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=IDS)
+@pytest.mark.parametrize("rows", [1, 9, 40, 140])
+def test_unwritten_blocks_beside_masked_large_ones(rows, dtype):
+    """The 64 keys in front are a masked block of values of 2^56 and blocks without any: their scores
+    stand for no value at all."""
+    c, g = make_cache([290], 2, 64, 16, max_seq=600)
+    c.grow([rows])
+    c.v_scale.fill_(2.0 ** -6)
+    c.k_scale.fill_(2.0 ** -6)
+    c.v_scale[0, pages_of(c, 0, 0, 16)] = 2.0 ** 56
+    c.v_scale[0, pages_of(c, 0, 16, 64)] = 0
+    q = (torch.randn(rows, 4, 64, generator=g) / 8).to(dtype).cuda()
+    bias = torch.randn(4, 300, generator=g).cuda()
+    bias[:, 275:] = -math.inf
+    check(c, q, [rows], 1.0, bias)
