@@ -421,7 +421,13 @@ int ssd_cache_load(const ssd_cache* cache, int rows, const int64_t* d_slot, void
  * without a position to attend, or whose scores are all -inf, gets zeros; a NaN score stays NaN in
  * its own row.  Rows of no sequence are left as they are.  A position past the table sets
  * SSD_DEV_CAPACITY (its keys end at the table's), as does a sequence of more than max_rows rows (the
- * further ones are left); a page outside the pools SSD_DEV_BAD_PAGE, its keys skipped. */
+ * further ones are left); a page outside the pools SSD_DEV_BAD_PAGE, its keys skipped.
+ *
+ * dtype is the type of q and out.  Codes and scales enter exactly, sums and the softmax's statistics are
+ * float32.  Held in fewer bits: elements of float32 queries to 2^-22 of themselves (those of either
+ * type to 2^-39 of their row's largest), the weights times their value scale to 2^-22 of themselves
+ * for float32 rows and 2^-11 for bf16 ones (an eighth of the output's own rounding), and to 2^-27 of the
+ * row's largest such product.  Weights under 2^-126 of the largest are zero. */
 typedef struct {
   int32_t B;          /* sequences, 1 .. 4096 */
   int32_t rows;       /* query rows in all; B * max_rows when row_start is NULL */
