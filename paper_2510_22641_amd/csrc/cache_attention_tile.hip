@@ -282,7 +282,7 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
 #pragma unroll
         for (int i = 1; i < TKEYS / 4; i += 2)  // (the last one twice)
           mx = max3(mx, s[t][i / 4][i % 4], s[t][(i + 1 < TKEYS / 4 ? i + 1 : i) / 4][(i + 1 < TKEYS / 4 ? i + 1 : i) % 4]);
-        mx = col_max(mx) * (BIAS ? 1.f : f);
+        mx = BIAS ? col_max(mx) : rounded(col_max(mx), f);
         float drop, num_drop;
         if (ref[t].move(mx, (float)vtop, drop, num_drop)) {  // rare once a few units are seen
           l[t] *= drop;
