@@ -51,9 +51,13 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
   // by unit modulo 3 (one in work, one to convert, one being written): scales over its largest
   __shared__ __attribute__((aligned(16))) float ksc[3][TKEYS], vsc[3][TKEYS];
   __shared__ __attribute__((aligned(16))) uint64_t rows[2][TKEYS];  // bytes from the pools' begin on, of the unit to load next
-  __shared__ uint64_t live[3];           // keys of the unit that have a row
-  __shared__ int tops[3], group[3][TKEYS];  // exponents of the largest key and value scale, each key's group's
-  __shared__ int apart[3];                  // whether the unit has several groups
+  struct Unit {
+    uint64_t live;  // keys that have a row
+    int top;        // exponents of the largest key and value scale
+    int apart;      // whether there are several groups
+  };
+  __shared__ __attribute__((aligned(16))) Unit facts[3];
+  __shared__ int group[3][TKEYS];  // exponents of each key's group
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 15, g = lane >> 4;
   const int hk = blockIdx.x % a.n_heads, bt = blockIdx.x / a.n_heads;
@@ -176,11 +180,7 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
     vsc[sc][lane] = ldexpf(1.f, ve - vt);
     group[sc][lane] = pair_of(kt, vt);
     const uint64_t in = __ballot(row != NO_ROW);
-    if (lane == 0) {
-      live[sc] = in;
-      tops[sc] = pair_of(kt, vt);
-      apart[sc] = far;
-    }
+    if (lane == 0) facts[sc] = Unit{in, pair_of(kt, vt), far};
   };
   auto store_row = [&](int buf, uint32_t row) {  // keys without a row read the pools' first: they are masked
     rows[buf][lane] = row == NO_ROW ? 0 : (uint64_t)row * DH;
@@ -210,6 +210,13 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
     __syncthreads();
   }
 
+  // (a unit's own is read before the barrier in front of it, and known to be the same in every lane)
+  auto unit_at = [&](int sc) {
+    const Unit u = facts[sc];
+    return Unit{uniform(u.live), uniform(u.top), uniform(u.apart)};
+  };
+  Unit unit = {};
+  if (x0 < x1) unit = unit_at(0);
   for (int x = x0, i0 = 0, i1 = 1, i2 = 2; x < x1; ++x) {
     const int buf = (x - x0) & 1;
     int page3 = -1;
@@ -220,14 +227,14 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
         page3 = entry(x + 3);
       }
     }
-    uint64_t rest = !idle && x * TKEYS <= wlast ? uniform(live[i0]) : 0;
+    uint64_t rest = !idle && x * TKEYS <= wlast ? unit.live : 0;
     while (rest) {
       // (one turn, but for rare units: what each turn loads and computes stays in it)
       int key0 = x * TKEYS;
       asm volatile("" : "+s"(key0) : : "memory");
       uint64_t in = rest;  // the keys of this turn
-      int top = uniform(tops[i0]);
-      if (uniform(apart[i0])) {
+      int top = unit.top;
+      if (unit.apart) {
         const int own = group[i0][lane];
         top = __builtin_amdgcn_readlane(own, __builtin_ctzll(rest));
         in &= __ballot(own == top);
@@ -348,6 +355,7 @@ __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const Cache
       }
     }
     if (x + 1 < x1) {
+      unit = unit_at(i1);
       convert(buf ^ 1, i1);
       if (wave == 0) {
         store_scales(i2, row2);
