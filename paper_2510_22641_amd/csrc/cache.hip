@@ -56,7 +56,7 @@ __device__ __forceinline__ int find_seq(const int* start, int B, int r) {
 // other blocks are writing.  Then a block writes its share of the new table entries and the slots
 // of its 256 rows, each finding its sequence by bisection in LDS.  Bound: launch latency and
 // one dependent chain (lengths, sums, table entry), not bytes (8 sequences 3.6 us, an empty kernel's;
-// 1024 with 83 thousand rows 8.1).
+// 1024 with 83 thousand rows 8.2).
 __global__ __launch_bounds__(MAP_THREADS) void page_map_kernel(const PageMapArgs a, const uint32_t ps_inv) {
   extern __shared__ int map_lds[];
   int* row0 = map_lds;               // [B + 1] first row of each sequence
@@ -235,7 +235,7 @@ constexpr int STORE_HELD = 8;  // passes of rows kept in registers between the m
 // (their codes times the old scale), rescales those where the block's scale changes, and writes the
 // run's codes; 32 (or 16) lanes take four elements each of a row.  Every block belongs to one wave,
 // so nothing is atomic.  Bound: bytes for long prompts (8192 bf16 rows of 32 heads of 128, K and V:
-// 201 MB in 49 us, 4.1 TB/s, where a large copy reaches 4.9); the chain slot -> rows, codes and
+// 201 MB in 50 us, 4.1 TB/s, where a large copy reaches 4.9; float32: 336 MB in 78, 4.3); the chain slot -> rows, codes and
 // scale -> reduction -> store for single tokens (29 float32 rows of 32 heads of 64: 5.0 us).
 template <typename T, int DH, bool VEC>
 __global__ __launch_bounds__(64 * STORE_WAVES) void cache_store_kernel(const CacheRowsArgs a, const int window,
@@ -395,7 +395,7 @@ __global__ __launch_bounds__(64 * STORE_WAVES) void cache_store_kernel(const Cac
 }
 
 // Rows back from their blocks: eight codes a lane, consecutive lanes on consecutive elements of a
-// row, K (blockIdx.y 0) or V.  Bound: bytes (the same rows: 201 MB in 43 us, 4.6 TB/s).
+// row, K (blockIdx.y 0) or V.  Bound: bytes (the same rows: 201 MB in 44 us, 4.5 TB/s; 336 in 69, 4.9).
 template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void cache_load_kernel(const CacheRowsArgs a) {
   const int per = a.n_heads * a.d_head / 8;  // lanes a row

@@ -41,9 +41,9 @@ __device__ __forceinline__ V scalar_load(const V* p) {
 // scales multiply the scores and the weights.  Each wave keeps its own references and sums; they
 // meet in LDS once.
 // Bound: for long contexts the bytes of the codes, which lie scattered in pieces of a page and head
-// (one token, 32 heads of 128 over 32768 positions: 269 MB in 52 us and 5 for the merge; 32 tokens of
-// 2048 positions, 8 cache heads: 134 MB in 33 us; of 1 to 4096: 130 MB in 41); for short ones the
-// chain lengths -> table -> codes (70 positions: 5.4 us, of which an empty kernel takes 3.9).
+// (one token, 32 heads of 128 over 32768 positions: 269 MB in 50 us and 5 for the merge; 32 tokens of
+// 2048 positions, 8 cache heads: 134 MB in 31 us; of 1 to 4096: 130 MB in 41); for short ones the
+// chain lengths -> table -> codes (70 positions: 5.5 us, of which an empty kernel takes 3.9).
 template <typename T, int DH, bool BIAS, bool EVEN, int AW>
 __global__ __launch_bounds__(64 * AW, DH == 64 && AW == 4 ? 3 : 2) void cache_attn_kernel(const CacheAttnArgs a, const int tiles,
                                                                                const int splits, const uint32_t ps_inv) {
@@ -369,11 +369,16 @@ __global__ __launch_bounds__(MERGE) void cache_attn_merge_kernel(const CacheAttn
 // (row, head) pairs of the longest sequence and cache head.
 long long pairs_of(const CacheAttnArgs& a) { return a.max_rows * (long long)(a.n_q_heads / a.n_heads); }
 
-// Pairs a block takes.  16 in the kernel above.  Beyond, the kernel for many rows: 64 in four waves of
-// one tile each; 128 in eight of one tile; 256 in eight of two where that leaves a block for every
-// compute unit, since two tiles share what is read from LDS (4096 bf16 rows of 32 heads over 8192
-// positions: 455 us against 640), but not for float32 rows of 128, whose two tiles' operands do not
-// fit the registers (three times 608 rows: 104 us against 39).
+// Pairs a block takes.  16 in the kernel above.  Beyond, the kernel for many rows:
+// * 64 in four waves of one tile each.  (Tiles of 16 of the kernel above measured between half and 1.1
+//   of its time.  Eight requests over 1000 positions, 17 to 64 float32 rows of 64 elements and a bias:
+//   17 to 22 us against 34 to 42; chunks of 6 to 21 bf16 rows of three heads over pages of seven: 17 to
+//   26 against 20 to 24.)
+// * 128 in eight waves of one tile (80 and 128 of the former rows: 56 and 59 us, in blocks of 64 49 and 51).
+// * 256 in eight waves of two tiles, which share what is read from LDS, where that leaves a block for every
+//   compute unit (4096 bf16 rows of 32 heads of 128 over 8192 positions: 484 us against 721 in blocks of
+//   128; 1000 of 64 over 3000: 97 either way; 300 float32 rows of 64 with a bias: 98 against 69); not
+//   for float32 rows of 128, whose two tiles' operands do not fit the registers.
 int block_pairs(const CacheAttnArgs& a) {
   const long long p = pairs_of(a);
   if (p <= 64) return p <= 16 ? 16 : 64;
@@ -397,8 +402,8 @@ hipError_t launch_t(const CacheAttnArgs& a, hipStream_t s) {
     const int tiles = (int)((pairs_of(a) + 15) / 16);
     const uint32_t inv = page_inv(a.page_size);
     // eight waves where that leaves each two units of the longest range (eight requests of up to 1000
-    // positions and nine rows each: 13.5 us against 15.4), four for shorter ones (70 positions: 5.7
-    // against 5.8)
+    // positions and nine rows each: 12.7 us against 15.3), four for shorter ones (70 positions: 5.5
+    // against 5.6; eight requests of 300, one row each: 7.6 against 7.0)
     const int waves = a.max_len / splits >= 16 * UNIT ? 8 : 4;
     const dim3 block(64 * waves);
 #define LAUNCH(BIAS, EVEN)                                                                                          \
@@ -421,10 +426,13 @@ hipError_t launch_t(const CacheAttnArgs& a, hipStream_t s) {
 
 // Key ranges a (row, head) pair's keys are split into: a block for each of the 256 compute units (two
 // of the 64-pair kernel's four waves), while a range keeps 128 keys.  More of them measured no
-// faster (one token of 32 heads over 32768 positions: 57 us with 256 blocks of eight waves, 60 with
-// 512; 32 tokens of 8 cache heads: 41 against 47).  The few-row kernel keeps short ranges whole, where
-// the merge would cost more than the waves save (one token of 32 heads of 128: 300 positions 8.7 us
-// whole, 9.6 in three ranges; 1000: 13.6 and 9.7 in eight; four tokens, 1000: 15.1 and 16.1 in two).
+// faster (one token of 32 heads over 32768 positions: 58 us with 256 blocks of eight waves, 61 with
+// 512; 32 tokens of 8 cache heads: 40 against 45).  The few-row kernel keeps short ranges whole, where
+// the merge would cost more than the waves save (one token of 32 heads of 128: 300 positions 8.0 us
+// whole, 9.3 in three ranges; 600: 8.7 and 9.2 in five; 1000: 11.3 and 9.1 in eight; two tokens, 1000:
+// 12.7 and 11.9 in four; four, 1000 and 1900: 13.3 and 18.3, 15.0 and 19.3 in two).  The rule counts
+// blocks alone: where there are enough of them, one long sequence among short ones is not split (one of
+// 32768 positions 58 us, seven of 100 beside it 212).
 int cache_attn_splits(const CacheAttnArgs& a) {
   const long long blocks = blocks_of(a);
   long long want = (256LL * (block_pairs(a) == 64 ? 2 : 1) + blocks - 1) / blocks;

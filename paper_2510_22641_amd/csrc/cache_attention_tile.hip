@@ -36,9 +36,9 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 // other, the others masked (scales in registers beside the scores would spill).
 // Bound: vector instructions of the softmax (about nine slots a score, four of them the
 // exponential) beside the matrix instructions (two a 16 x 16 x 32 piece for bf16 rows, four for
-// float32).  4096 bf16 rows of 32 heads of 128 behind 4096 positions: 412 GFLOP in 457 us, 0.90
+// float32).  4096 bf16 rows of 32 heads of 128 behind 4096 positions: 412 GFLOP in 484 us, 0.85
 // PFLOP/s, the vector instructions busy for half of the time and the matrix instructions for a
-// third.  Few units a block are round trips: three times 608 float32 rows 38 us, ragged chunks of 17
+// third.  Few units a block are round trips: three times 608 float32 rows 39 us, ragged chunks of 17
 // rows over up to 2777 positions 18 us.
 template <typename T, int DH, bool BIAS, int NT, int TW>
 __global__ __launch_bounds__(64 * TW, 2) void cache_attn_tile_kernel(const CacheAttnArgs a, const int tiles,

@@ -34,7 +34,7 @@ class PagedCache:
     page and head (``ssd_cache``), a page table, and the pages not yet in use.
 
     ``grow`` gives sequences new positions, ``append`` stores their rows, ``attend`` attends them
-    and ``rows`` reads them back.  All run on torch's current stream of the device, whichever device
+    and ``rows`` reads them back.  It only grows: pages are not given back.  All run on torch's current stream of the device, whichever device
     is current; their tensors must have been made or waited for on that stream.
     """
 
